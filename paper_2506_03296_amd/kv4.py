@@ -1,0 +1,280 @@
+"""Python binding of libapex_kv4.so: a 4-bit paged KV cache on MI355X.
+
+Argument marshalling only, as in the package's decode-attention binding; the
+names and semantics follow include/apex_kv4.h.
+
+    cache = kv4.empty_cache(num_blocks, Hkv, device)         # uint8 [num_blocks][Hkv][2176]
+    kv4.append(k_new, v_new, cache, slot_mapping)            # fp16 rows in, quantised
+    out = kv4.attention(q, cache, block_table, context_lens, scale, lse_out=lse)
+    kv4.accumulate_weights(q, cache, block_table, context_lens, scale, lse, weights)
+    kv4.evict(cache, block_table, context_lens, weights, positions, keep, sinks, recent)
+    k, v = kv4.gather(cache, slot_mapping)                   # fp16 rows back
+
+block_table int32 [B][entries per row], context_lens int32 [B]; weights fp32
+and positions int32, both [num_blocks][Hkv][16], belong to the cached tokens.
+All tensors are on one GPU; a call works on that device's current stream.
+"""
+import ctypes
+import os
+
+from . import APEX_ERR_HIP, APEX_OK, ApexError, _on, _raw_stream, _require, _torch
+
+__all__ = ["LIB_PATH", "EXPORTED_SYMBOLS", "SLAB_BYTES", "BLOCK_SIZE", "HEAD_DIM", "load_library", "last_error",
+           "empty_cache", "append", "gather", "attention", "accumulate_weights", "evict",
+           "attention_workspace_bytes", "attention_counter_bytes", "evict_workspace_bytes", "release_workspace"]
+
+LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libapex_kv4.so")
+EXPORTED_SYMBOLS = (
+    "apex_kv4_append", "apex_kv4_gather", "apex_kv4_attention", "apex_kv4_attention_workspace_bytes",
+    "apex_kv4_attention_counter_bytes", "apex_kv4_accumulate_weights", "apex_kv4_evict",
+    "apex_kv4_evict_workspace_bytes", "apex_kv4_last_error", "apex_kv4_release_workspace",
+)
+SLAB_BYTES = 2176
+BLOCK_SIZE = 16
+HEAD_DIM = 128
+
+_LIB = None
+
+
+def load_library(path=None):
+    """Load (once) and return the ctypes handle of libapex_kv4.so."""
+    global _LIB
+    if _LIB is not None and path is None:
+        return _LIB
+    p = path or LIB_PATH
+    try:
+        import torch  # noqa: F401  (its HIP runtime is the one to bind to)
+    except ImportError:
+        pass
+    if not os.path.exists(p):
+        raise ApexError(APEX_ERR_HIP, f"{p} is not built; run __graft_entry__.build() "
+                                      "(python -m paper_2506_03296_amd.build)")
+    lib = ctypes.CDLL(p)
+    vp, i32, i64, f32, size = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+    for name, res, args in (
+            ("apex_kv4_append", i32, [vp, vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, i64, vp]),
+            ("apex_kv4_gather", i32, [vp, vp, vp, vp, i32, i32, i32, i32, i64, vp]),
+            ("apex_kv4_attention", i32, [vp, vp, vp, i64, vp, vp, vp, i32, i32, i32, i32, i32, i64, f32, vp, size, vp]),
+            ("apex_kv4_attention_workspace_bytes", size, [i32, i32, i32]),
+            ("apex_kv4_attention_counter_bytes", size, [i32, i32]),
+            ("apex_kv4_accumulate_weights", i32, [vp, vp, vp, i64, vp, vp, vp, i32, i32, i32, i32, i32, i64, f32, vp]),
+            ("apex_kv4_evict", i32, [vp, vp, i64, vp, vp, vp, i32, i32, i32, i32, i64, i32, i32, i32, vp, size, vp]),
+            ("apex_kv4_evict_workspace_bytes", size, [i32, i32, i64]),
+            ("apex_kv4_last_error", ctypes.c_char_p, []),
+            ("apex_kv4_release_workspace", i32, [])):
+        f = getattr(lib, name)
+        f.restype, f.argtypes = res, args
+    if path is None:
+        _LIB = lib
+    return lib
+
+
+def last_error():
+    return load_library().apex_kv4_last_error().decode()
+
+
+def _check(rc):
+    if rc != APEX_OK:
+        raise ApexError(rc, last_error())
+
+
+def _call(name, index, *args):
+    """The entry point, with the tensors' device (its index) current."""
+    f = getattr(load_library(), name)
+    cuda = _torch().cuda
+    if cuda.current_device() == index:
+        rc = f(*args)
+    else:
+        with cuda.device(index):
+            rc = f(*args)
+    if rc:
+        _check(rc)
+
+
+def release_workspace():
+    _check(load_library().apex_kv4_release_workspace())
+
+
+def attention_workspace_bytes(B, Hq, Hkv):
+    """Bytes of an attention workspace on the current device (0: bad shapes)."""
+    return int(load_library().apex_kv4_attention_workspace_bytes(B, Hq, Hkv))
+
+
+def attention_counter_bytes(B, Hkv):
+    return int(load_library().apex_kv4_attention_counter_bytes(B, Hkv))
+
+
+def evict_workspace_bytes(B, Hkv, block_table_stride):
+    return int(load_library().apex_kv4_evict_workspace_bytes(B, Hkv, block_table_stride))
+
+
+def empty_cache(num_blocks, Hkv, device):
+    """An uninitialised cache for num_blocks blocks of 16 tokens."""
+    torch = _torch()
+    return torch.empty((num_blocks, Hkv, SLAB_BYTES), dtype=torch.uint8, device=device)
+
+
+def _ready(t, dtype, shape, index):
+    """True if t is a contiguous tensor of this dtype and shape on GPU `index`."""
+    return t.dtype is dtype and t.shape == shape and t.is_cuda and t.get_device() == index and t.is_contiguous()
+
+
+def _want(t, name, dtype, shape, device):
+    """As _ready, with an error for what is not so."""
+    if not _ready(t, dtype, shape, device.index):
+        _require(t, name, dtype, device, shape=shape)
+
+
+def _cache(kv_cache):
+    """(num_blocks, Hkv, device, index) of a cache."""
+    torch = _torch()
+    shape = kv_cache.shape
+    if len(shape) != 3 or shape[2] != SLAB_BYTES:
+        raise ValueError(f"kv_cache must be [num_blocks][Hkv][{SLAB_BYTES}], got {tuple(shape)}")
+    if not kv_cache.is_cuda:
+        raise ValueError(f"kv_cache must be a GPU tensor, got {kv_cache.device}")
+    if kv_cache.dtype is not torch.uint8 or not kv_cache.is_contiguous():
+        _require(kv_cache, "kv_cache", torch.uint8, kv_cache.device)
+    return shape[0], shape[1], kv_cache.device, kv_cache.get_device()
+
+
+def _batch(block_table, context_lens, device):
+    """(B, entries per table row)."""
+    i32 = _torch().int32
+    if block_table.dim() != 2:
+        raise ValueError(f"block_table must be [B][entries per row], got {tuple(block_table.shape)}")
+    B, stride = block_table.shape
+    _want(block_table, "block_table", i32, (B, stride), device)
+    _want(context_lens, "context_lens", i32, (B,), device)
+    return B, stride
+
+
+def _queries(q, B, Hkv, device):
+    """Hq."""
+    if q.dim() != 3 or q.shape[0] != B or q.shape[2] != HEAD_DIM:
+        raise ValueError(f"q must be [B={B}][Hq][{HEAD_DIM}], got {tuple(q.shape)}")
+    _want(q, "q", _torch().float16, q.shape, device)
+    return q.shape[1]
+
+
+def _workspace(workspace, device):
+    if workspace is None:
+        return None, 0
+    if not (_on(workspace, _torch().uint8, device.index) and workspace.is_contiguous()):
+        _require(workspace, "workspace", _torch().uint8, device)
+    return workspace.data_ptr(), workspace.numel()
+
+
+def append(k_new, v_new, kv_cache, slot_mapping, token_positions=None, positions=None, weights=None, stream=None):
+    """apex_kv4_append over torch tensors (in place on the cache).
+
+    k_new/v_new: fp16 [T][Hkv][128] with unit strides inside a token (the token
+    stride may be wider, e.g. views into a fused QKV buffer, but must be the
+    same for both); slot_mapping int64 [T] (negative = padding);
+    token_positions int32 [T] go to ``positions``; ``weights`` of the slots
+    become 0."""
+    torch = _torch()
+    nb, Hkv, dev, index = _cache(kv_cache)
+    if k_new.dim() != 3 or v_new.shape != k_new.shape or k_new.shape[1] != Hkv or k_new.shape[2] != HEAD_DIM:
+        raise ValueError(f"k_new and v_new must both be [T][Hkv={Hkv}][{HEAD_DIM}]")
+    T = k_new.shape[0]
+    if not (_on(k_new, torch.float16, index) and _on(v_new, torch.float16, index)):
+        _require(k_new, "k_new", torch.float16, dev, contiguous=False)
+        _require(v_new, "v_new", torch.float16, dev, contiguous=False)
+    ks, vs = k_new.stride(), v_new.stride()
+    if ks[2] != 1 or vs[2] != 1 or (Hkv > 1 and (ks[1] != HEAD_DIM or vs[1] != HEAD_DIM)):
+        raise ValueError("each token's rows must be contiguous [Hkv][d]")
+    if T > 1 and ks[0] != vs[0]:
+        raise ValueError("k_new and v_new must share the token stride")
+    _want(slot_mapping, "slot_mapping", torch.int64, (T,), dev)
+    if (positions is None) != (token_positions is None):
+        raise ValueError("positions and token_positions go together")
+    if positions is not None:
+        _want(token_positions, "token_positions", torch.int32, (T,), dev)
+        _want(positions, "positions", torch.int32, (nb, Hkv, BLOCK_SIZE), dev)
+    if weights is not None:
+        _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev)
+    _call("apex_kv4_append", index, k_new.data_ptr(), v_new.data_ptr(), ks[0] if T > 1 else 0, kv_cache.data_ptr(),
+          slot_mapping.data_ptr(), None if positions is None else token_positions.data_ptr(),
+          None if positions is None else positions.data_ptr(), None if weights is None else weights.data_ptr(),
+          T, Hkv, HEAD_DIM, BLOCK_SIZE, nb, _raw_stream(stream, index))
+
+
+def gather(kv_cache, slot_mapping, k_out=None, v_out=None, stream=None):
+    """apex_kv4_gather over torch tensors; returns (k_out, v_out), fp16
+    [T][Hkv][128]: the values of the slots (int64 [T]), zeros for a slot outside
+    the pool."""
+    torch = _torch()
+    nb, Hkv, dev, index = _cache(kv_cache)
+    T = slot_mapping.numel()
+    _want(slot_mapping, "slot_mapping", torch.int64, (T,), dev)
+    shape = (T, Hkv, HEAD_DIM)
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=torch.float16, device=dev)
+    else:
+        _want(k_out, "k_out", torch.float16, shape, dev)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=torch.float16, device=dev)
+    else:
+        _want(v_out, "v_out", torch.float16, shape, dev)
+    _call("apex_kv4_gather", index, kv_cache.data_ptr(), slot_mapping.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+          T, Hkv, HEAD_DIM, BLOCK_SIZE, nb, _raw_stream(stream, index))
+    return k_out, v_out
+
+
+def attention(q, kv_cache, block_table, context_lens, scale, out=None, lse_out=None, workspace=None, stream=None):
+    """apex_kv4_attention over torch tensors; returns ``out``.
+
+    ``workspace`` is an optional uint8 tensor of attention_workspace_bytes(B,
+    Hq, Hkv) bytes whose first attention_counter_bytes(B, Hkv) are zero (e.g.
+    from torch.zeros); calls that can overlap, and a captured graph, need one
+    of their own."""
+    torch = _torch()
+    nb, Hkv, dev, index = _cache(kv_cache)
+    B, stride = _batch(block_table, context_lens, dev)
+    Hq = _queries(q, B, Hkv, dev)
+    if out is None:
+        out = torch.empty((B, Hq, HEAD_DIM), dtype=torch.float16, device=dev)
+    else:
+        _want(out, "out", torch.float16, q.shape, dev)
+    if lse_out is not None:
+        _want(lse_out, "lse_out", torch.float32, (B, Hq), dev)
+    ws, ws_bytes = _workspace(workspace, dev)
+    _call("apex_kv4_attention", index, q.data_ptr(), kv_cache.data_ptr(), block_table.data_ptr(), stride,
+          context_lens.data_ptr(), out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), B, Hq, Hkv,
+          HEAD_DIM, BLOCK_SIZE, nb, scale, ws, ws_bytes, _raw_stream(stream, index))
+    return out
+
+
+def accumulate_weights(q, kv_cache, block_table, context_lens, scale, lse, weights, stream=None):
+    """apex_kv4_accumulate_weights over torch tensors (in place on ``weights``);
+    ``lse`` fp32 [B][Hq] is the ``lse_out`` of the step's attention."""
+    torch = _torch()
+    nb, Hkv, dev, index = _cache(kv_cache)
+    B, stride = _batch(block_table, context_lens, dev)
+    Hq = _queries(q, B, Hkv, dev)
+    _want(lse, "lse", torch.float32, (B, Hq), dev)
+    _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev)
+    _call("apex_kv4_accumulate_weights", index, q.data_ptr(), kv_cache.data_ptr(), block_table.data_ptr(), stride,
+          context_lens.data_ptr(), lse.data_ptr(), weights.data_ptr(), B, Hq, Hkv, HEAD_DIM, BLOCK_SIZE, nb, scale,
+          _raw_stream(stream, index))
+
+
+def evict(kv_cache, block_table, context_lens, weights, positions, keep, sinks=0, recent=0, workspace=None,
+          stream=None):
+    """apex_kv4_evict over torch tensors (in place on the cache, ``weights`` and
+    ``positions``).  A request longer than ``keep`` has the length ``keep``
+    afterwards; context_lens is left to the caller.
+
+    ``workspace`` is an optional uint8 tensor of evict_workspace_bytes(B, Hkv,
+    block_table.shape[1]) bytes; calls that can overlap, and a captured graph,
+    need one of their own."""
+    torch = _torch()
+    nb, Hkv, dev, index = _cache(kv_cache)
+    B, stride = _batch(block_table, context_lens, dev)
+    _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev)
+    _want(positions, "positions", torch.int32, (nb, Hkv, BLOCK_SIZE), dev)
+    ws, ws_bytes = _workspace(workspace, dev)
+    _call("apex_kv4_evict", index, kv_cache.data_ptr(), block_table.data_ptr(), stride, context_lens.data_ptr(),
+          weights.data_ptr(), positions.data_ptr(), B, Hkv, HEAD_DIM, BLOCK_SIZE, nb, keep, sinks, recent, ws, ws_bytes,
+          _raw_stream(stream, index))
