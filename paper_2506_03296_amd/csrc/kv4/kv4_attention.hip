@@ -33,13 +33,8 @@
 
 namespace {
 
-using apex::AttnParams;
 using apex::f16;
 using apex::f32x4;
-using apex::kAttnThreads;
-using apex::kStageFloats;
-using apex::kWaves;
-using apex::RowState;
 using apex::u32x2;
 using apex::u32x4;
 using apex::uniform;
@@ -51,36 +46,68 @@ using kv4::kSlabBytes;
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// Cost of starting and finishing a pair, in blocks.
-constexpr int kPairCost = 24;
+// Eight waves per work group and one work group per CU: they keep 4 blocks, 70
+// KiB a CU, on their way, and 25 KiB saturate the memory.  More waves would need
+// registers that the loop has not got (with 4 per SIMD it spills: 97 us for the
+// 213 000 slabs of 32 requests of 4096-32768 tokens, 75 with 2).
+constexpr int kThreads = 512;
+constexpr int kWaves = kThreads / 64;
 
-struct Kv4Params {
+struct Params {
+    const f16* q;           // [B][Hq][128]
     const char* cache;      // [num_blocks][Hkv][kSlabBytes]
-    const int32_t* bt;
+    const int32_t* bt;      // [B][stride]
     const int32_t* lens;
-    int64_t num_blocks;
-    int stride;             // entries per table row
-    int workers;            // work groups that may get units
+    unsigned num_blocks;
+    int stride;
+    int B, Hq, Hkv;
+    int workers;            // work groups launched
     float scale_log2;       // |scale| log2(e)
     unsigned q_sign;        // 0x8000 to negate q (scale < 0)
-    const float* lse_in;    // accumulation of the weights: [B][Hq], and
+    // attention
+    f16* out;
+    float* lse;             // may be null
+    int32_t* counters;      // [B][Hkv] arrivals, zero between calls
+    float* pacc;            // [2 workers][G][128] partial sums of the weighted values,
+    float* pml;             // [2 workers][G][2] their maxima (log2 units) and sums of weights
+    // accumulation of the weights
+    const float* lse_in;    // [B][Hq]
     float* weights;         // [num_blocks][Hkv][16]
 };
 
 // --- partition ----------------------------------------------------------------
 //
-// The line of plan_policy.h: every non-empty (request, kv-head) pair has K cost
-// positions, then its blocks; work group w takes positions [start(w),
-// start(w + 1)).  Every wave derives it on its own from context_lens: a lane
-// sums ceil(B / 64) consecutive requests, one scan joins them.  All positions
-// are below 2^31 (the host checks the table's size).
+// Every wave derives the work group's share on its own from context_lens: a lane
+// sums ceil(B / 64) consecutive requests, one scan joins them.  Three ways:
+//   whole   many short pairs: a wave takes whole (request, kv-head) pairs;
+//   parts   few pairs: each is cut into equal parts, a work group takes one part;
+//   line    else: the line of plan_policy.h: every non-empty pair has kPairCost
+//           positions, then its blocks; work group w takes the positions
+//           [start(w), start(w + 1)).
+// All positions are below 2^31 (the host checks the table's size).
+
+// What starting and finishing a pair costs a work group, in blocks: about 3 us,
+// where a block takes 0.08.
+constexpr unsigned kPairCost = 32;
+// Parts: the least, and the most that still goes better than the line (uneven
+// last parts against pairs that begin and end inside a work group).
+constexpr unsigned kMinPart = 32, kMaxPart = 320;
+// Whole pairs by waves: at most this many blocks.
+constexpr unsigned kWholeBlocks = 32;
 
 struct Line {
     unsigned V, W, per, rest;   // positions, work groups; V = W per + rest
+    __device__ inline void set(unsigned positions, unsigned groups)
+    {
+        V = positions;
+        W = groups;
+        per = W ? V / W : 0;
+        rest = V - per * W;
+    }
     __device__ inline unsigned start(unsigned w) const { return w * per + w * rest / W; }   // (w rest < W^2)
     __device__ inline unsigned owner(unsigned v) const
     {
-        // w is at most one off the quotient of the reals
+        // at most one off the quotient of the reals
         unsigned w = (unsigned)((double)v * (double)W / (double)V);
         if (w >= W) w = W - 1;
         while (w + 1 < W && start(w + 1) <= v) ++w;
@@ -89,71 +116,144 @@ struct Line {
     }
 };
 
+enum Way { kLine, kParts, kWhole };
+
 struct Plan {
+    Way way;
     Line line;
-    unsigned v0, v1;        // the work group's positions
-    int b, g, blk, L;       // its first segment
-    unsigned vf;            // position of the pair's block 0
+    unsigned v1;            // line: end of the work group's positions
+    unsigned vf;            // line: position of the pair's block 0
+    int b, g, blk, L;       // the first segment
+    int take;               // its blocks; 0: none
+    int first, last;        // parts: the work groups of the pair
     bool empty_rows;        // some request has no context
 };
 
-__device__ inline int cut_len(const Kv4Params& p, int L)
+__device__ inline int context(const Params& p, int b)
 {
     const int64_t row = (int64_t)p.stride * kBlockSize;
+    const int L = p.lens[b];
     return L > row ? (int)row : L;
 }
 
 __device__ inline unsigned blocks(int L) { return L > 0 ? ((unsigned)L + kBlockSize - 1) / kBlockSize : 0u; }
 
-__device__ inline Plan make_plan(const Kv4Params& p, int B, int Hkv, unsigned K, unsigned w, int lane)
+// Blocks per part of a pair of nb; a long pair takes longer ones, since the last
+// work group to finish reads all the parts' partials.
+__device__ inline unsigned part_blocks(unsigned nb, unsigned least)
 {
-    const int R = (B + 63) / 64;
-    const int r0 = min(B, lane * R), r1 = min(B, r0 + R);
-    unsigned cost = 0, count = 0;
+    const unsigned t = max(kMinPart, kMinPart / 2 + nb / 64);
+    return max(t, least);
+}
+
+template <bool kAttention>
+__device__ inline Plan make_plan(const Params& p, unsigned K, unsigned w, int lane)
+{
+    const int R = (p.B + 63) / 64;
+    const int r0 = min(p.B, lane * R), r1 = min(p.B, r0 + R);
+    unsigned units = 0, count = 0, longest = 0;
     for (int b = r0; b < r1; ++b) {
-        const unsigned nb = blocks(cut_len(p, p.lens[b]));
+        const unsigned nb = blocks(context(p, b));
+        units += nb;
         count += nb > 0;
-        cost += nb > 0 ? nb + K : 0u;
+        longest = max(longest, nb);
     }
-    const unsigned hk = (unsigned)Hkv;
+    const unsigned hk = (unsigned)p.Hkv;
+    const unsigned cost = units + K * count;
     const unsigned hi = (unsigned)apex::wave_incl_sum((int)cost), lo = hi - cost;
     const unsigned total = (unsigned)apex::lane_value((int)hi, 63);
     const unsigned nonempty = (unsigned)apex::lane_value(apex::wave_incl_sum((int)count), 63);
+    longest = (unsigned)apex::lane_value(apex::wave_incl_max((int)longest), 63);
     Plan r;
-    r.empty_rows = nonempty < (unsigned)B;
-    r.v0 = r.v1 = r.vf = 0;
-    r.b = r.g = r.blk = r.L = 0;
-    const unsigned V = total * hk, pairs = nonempty * hk, U = V - K * pairs;
-    unsigned W = U / 8;   // at least two blocks a wave
-    W = W < pairs ? pairs : W;
-    W = W < (unsigned)p.workers ? W : (unsigned)p.workers;
-    r.line.V = V;
-    r.line.W = W;
-    if (V == 0 || w >= W) return r;
-    r.line.per = V / W;
-    r.line.rest = V - r.line.per * W;
-    r.v0 = r.line.start(w);
+    r.way = kLine;
+    r.empty_rows = nonempty < (unsigned)p.B;
+    r.v1 = r.vf = 0;
+    r.b = r.g = r.blk = r.L = r.take = r.first = r.last = 0;
+    const unsigned V = total * hk, pairs = nonempty * hk, U = V - K * pairs, W = (unsigned)p.workers;
+    r.line.set(V, W);
+    if (U == 0) return r;
+    if (kAttention && pairs > W && longest <= kWholeBlocks) {
+        r.way = kWhole;
+        return r;
+    }
+    if (kAttention && pairs <= W) {
+        const unsigned room = W - pairs;
+        const unsigned least = longest <= 2 * kMinPart ? longest : room > 0 ? (U + room - 1) / room : U;
+        if (least <= kMaxPart) {
+            // the parts of the requests before a lane's, then the request of part w
+            unsigned parts = 0;
+            for (int b = r0; b < r1; ++b) {
+                const unsigned nb = blocks(context(p, b));
+                const unsigned t = part_blocks(nb, least);
+                parts += (nb + t - 1) / t;
+            }
+            r.way = kParts;
+            const unsigned phi = (unsigned)apex::wave_incl_sum((int)parts), plo = phi - parts;
+            const uint64_t hit = __ballot(plo * hk <= w && w < phi * hk);
+            if (hit == 0) return r;
+            const int ln = __builtin_ctzll(hit);
+            unsigned rest = w - (unsigned)apex::lane_value((int)plo, ln) * hk;
+            unsigned nb, t, c;
+            for (int b = ln * R;; ++b) {
+                r.b = b;
+                r.L = uniform(context(p, b));
+                nb = blocks(r.L);
+                t = part_blocks(nb, least);
+                c = (nb + t - 1) / t;
+                if (rest < c * hk) break;
+                rest -= c * hk;
+            }
+            r.g = (int)(rest / c);
+            const unsigned part = rest - (unsigned)r.g * c;
+            // equal parts (which may leave the last work groups of the pair without one)
+            t = (nb + c - 1) / c;
+            r.blk = (int)min(nb, part * t);
+            r.take = (int)min(t, nb - (unsigned)r.blk);
+            r.first = (int)(w - part);
+            r.last = r.first + (int)((nb + t - 1) / t) - 1;
+            return r;
+        }
+    }
+    const unsigned v0 = r.line.start(w);
     r.v1 = r.line.start(w + 1);
+    if (v0 >= r.v1) return r;
     // the lane whose requests hold v0, then the request
-    const uint64_t hit = __ballot(lo * hk <= r.v0 && r.v0 < hi * hk);
-    const int ln = __builtin_ctzll(hit);
+    const int ln = __builtin_ctzll(__ballot(lo * hk <= v0 && v0 < hi * hk));
     unsigned at = (unsigned)apex::lane_value((int)lo, ln) * hk;
-    int b = ln * R;
     unsigned nb;
-    while (true) {
-        r.L = uniform(cut_len(p, p.lens[b]));
+    for (int b = ln * R;; ++b) {
+        r.b = b;
+        r.L = uniform(context(p, b));
         nb = blocks(r.L);
         const unsigned span = nb > 0 ? (nb + K) * hk : 0u;
-        if (r.v0 < at + span) break;
+        if (v0 < at + span) break;
         at += span;
-        ++b;
     }
-    r.b = b;
-    const unsigned off = r.v0 - at, len = nb + K;
+    const unsigned off = v0 - at, len = nb + K;
     r.g = (int)(off / len);
     r.vf = at + (unsigned)r.g * len + K;
-    r.blk = r.v0 > r.vf ? (int)(r.v0 - r.vf) : 0;
+    r.blk = v0 > r.vf ? (int)(v0 - r.vf) : 0;
+    if (r.vf + (unsigned)r.blk < r.v1) r.take = (int)min(nb - (unsigned)r.blk, r.v1 - (r.vf + (unsigned)r.blk));
     return r;
+}
+
+// Moves a line's plan to the work group's next segment; false when it has none.
+__device__ inline bool next_segment(const Params& p, unsigned K, Plan& r)
+{
+    const unsigned nb = blocks(r.L);
+    if ((unsigned)(r.blk + r.take) < nb) return false;   // the range ended inside the pair
+    r.vf += nb + K;
+    r.blk = 0;
+    if (r.vf >= r.v1) return false;
+    if (++r.g == p.Hkv) {
+        r.g = 0;
+        do {
+            if (++r.b >= p.B) return false;
+            r.L = uniform(context(p, r.b));
+        } while (r.L <= 0);
+    }
+    r.take = (int)min(blocks(r.L), r.v1 - r.vf);
+    return true;
 }
 
 // --- operands -----------------------------------------------------------------
@@ -169,7 +269,7 @@ struct QueryOperand {
 };
 
 template <int G>
-__device__ inline void load_query(const AttnParams& p, unsigned q_sign, int b, int g, int lane, QueryOperand<G>& op)
+__device__ inline void load_query(const Params& p, int b, int g, int lane, QueryOperand<G>& op)
 {
     const int col = lane & 15, q = lane >> 4;
     const int head = G == 8 ? col & 7 : (col & 3) & (G - 1);
@@ -182,7 +282,7 @@ __device__ inline void load_query(const AttnParams& p, unsigned q_sign, int b, i
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            w[i][j] ^= q_sign * 0x10001u;
+            w[i][j] ^= p.q_sign * 0x10001u;
             m = max(m, max(w[i][j] & 0x7fffu, (w[i][j] >> 16) & 0x7fffu));
         }
     // as floats the bit patterns of non-negative values order alike; a NaN or
@@ -222,18 +322,23 @@ struct Tile {
     unsigned vs;    // scale bytes of tokens 4q .. 4q + 3, group (lane % 16) / 4
 };
 
-template <bool kValues>
-__device__ inline void load_tile(Tile& t, const char* slab, int bytes, int lane)
+__device__ inline __amdgpu_buffer_rsrc_t slab_resource(const char* slab, int bytes)
 {
-    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)apex::uniform_ptr(slab), (short)0, bytes,
-                                                                       apex::kRawBufferWord3);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)apex::uniform_ptr(slab), (short)0, bytes, apex::kRawBufferWord3);
+}
+
+__device__ inline void load_keys(Tile& t, __amdgpu_buffer_rsrc_t r, int lane)
+{
     const int c = lane & 15, q = lane >> 4;
     t.k = __builtin_amdgcn_raw_buffer_load_b128(r, c * 64 + q * 16, 0, apex::kStreamingLoad);
     t.ks = __builtin_amdgcn_raw_buffer_load_b8(r, kv4::kKScales + c * 4 + q, 0, apex::kStreamingLoad);
-    if (kValues) {
-        t.v = __builtin_amdgcn_raw_buffer_load_b128(r, kv4::kVCodes + lane * 16, 0, apex::kStreamingLoad);
-        t.vs = __builtin_amdgcn_raw_buffer_load_b32(r, kv4::kVScales + (c >> 2) * 16 + q * 4, 0, apex::kStreamingLoad);
-    }
+}
+
+__device__ inline void load_values(Tile& t, __amdgpu_buffer_rsrc_t r, int lane)
+{
+    const int c = lane & 15, q = lane >> 4;
+    t.v = __builtin_amdgcn_raw_buffer_load_b128(r, kv4::kVCodes + lane * 16, 0, apex::kStreamingLoad);
+    t.vs = __builtin_amdgcn_raw_buffer_load_b32(r, kv4::kVScales + (c >> 2) * 16 + q * 4, 0, apex::kStreamingLoad);
 }
 
 // A value plus that of the lane 8 (or 4) columns on, within 16 lanes.
@@ -278,11 +383,12 @@ struct Span {
     int L;
 };
 
-__device__ inline Span wave_span(const Kv4Params& p, int b, int g, int L, int lo, int hi, int wave)
+// The wave's share of blocks [lo, hi), one of n (blocks are taken in twos).
+__device__ inline Span wave_span(const Params& p, int b, int g, int L, int lo, int hi, int i, int n)
 {
     Span s;
-    const int per = (hi - lo + kWaves - 1) / kWaves;
-    s.first = uniform(lo + wave * per);
+    const int per = (hi - lo + 2 * n - 1) / (2 * n) * 2;
+    s.first = uniform(lo + i * per);
     s.n = uniform(max(0, min(hi, s.first + per) - s.first));
     s.bt = p.bt + (size_t)uniform(b) * (size_t)p.stride + (s.n > 0 ? s.first : 0);
     s.pair = apex::uniform_ptr(p.cache + (size_t)uniform(g) * kSlabBytes);
@@ -290,127 +396,171 @@ __device__ inline Span wave_span(const Kv4Params& p, int b, int g, int L, int lo
     return s;
 }
 
-constexpr int kDepth = 4;   // blocks in flight per wave
+// Blocks of a wave are taken two at a time (a step), two steps in flight.
+struct Step {
+    Tile t[2];
+    unsigned id[2];     // block ids of the tiles,
+    unsigned next[2];   // and of those that refill them
+};
 
 template <int G>
-__device__ inline void attend(const Kv4Params& p, int Hkv, const Span& s, const QueryOperand<G>& op, int lane, State& st)
+__device__ inline void attend(const Params& p, int b, int g, const Span& s, int lane, State& st)
 {
     const int col = lane & 15, q = lane >> 4;
     const int parity = G == 8 ? col >> 3 : (col >> 2) & 1;
     // bytes 2 and 3 of a weight to the half of its parity, zeros to the other
     const unsigned place = parity ? 0x03020c0cu : 0x0c0c0302u;
     const unsigned low_part = G < 8 && col >= 8 ? 0xffff0000u : 0u;
-    const uint64_t step = (uint64_t)Hkv * kSlabBytes;
+    const uint64_t step_bytes = (uint64_t)p.Hkv * kSlabBytes;
+    const unsigned pool = p.num_blocks;
 
-    auto id_at = [&](int i) -> int {
-        return i < s.n ? *(const __attribute__((address_space(4))) int32_t*)(s.bt + i) : -1;
+    // (an entry that is not the wave's is replaced, not read: s.bt[0] is readable)
+    auto id_at = [&](int i) -> unsigned {
+        const unsigned id = *(const __attribute__((address_space(4))) uint32_t*)(s.bt + (i < s.n ? i : 0));
+        return i < s.n ? id : 0xffffffffu;
     };
-    auto ok = [&](int id) -> bool { return id >= 0 && (int64_t)id < p.num_blocks; };
-    auto load = [&](Tile& t, int id) {
-        const bool good = ok(id);
-        load_tile<true>(t, s.pair + (good ? (uint64_t)(uint32_t)id * step : 0), good ? kSlabBytes : 0, lane);
+    // the slab of a block, with no extent (loads give zeros) outside the pool
+    auto slab = [&](unsigned id) {
+        return slab_resource(s.pair + id * step_bytes, id < pool ? kSlabBytes : 0);
     };
     st.m = -INFINITY;
     st.l = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) st.acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    Tile tile[kDepth];
-    int id[kDepth], next[kDepth];
+    Step x[2];
 #pragma unroll
-    for (int i = 0; i < kDepth; ++i) {
-        id[i] = id_at(i);
-        load(tile[i], id[i]);
-        next[i] = id_at(kDepth + i);
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            x[i].id[j] = id_at(2 * i + j);
+            const auto r = slab(x[i].id[j]);
+            load_keys(x[i].t[j], r, lane);
+            load_values(x[i].t[j], r, lane);
+            x[i].next[j] = id_at(4 + 2 * i + j);
+        }
     }
 
-    auto block = [&](Tile& t, int k, int& id, int& next) {
-        const bool good = ok(id);
-        const int tok = (s.first + k) * kBlockSize + 4 * q;
-        const bool tail = !good || (s.first + k) * kBlockSize > s.L - kBlockSize;
-        f32x4 sc = scores<G>(t, op);
-        const u32x4 v = t.v;
-        const unsigned vs = t.vs;
-        id = next;
-        next = id_at(k + 2 * kDepth);
-        float vscale[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            vscale[e] = __uint_as_float((e == 0 ? vs << 23 : e == 1 ? vs << 15 : e == 2 ? vs << 7 : vs >> 1) & 0x7f800000u);
-        }
-        bool live[4];
-        if (tail) {
+    // q's digits are worked out while the first blocks are on their way
+    QueryOperand<G> op;
+    load_query<G>(p, b, g, lane, op);
+
+    // blocks k and k + 1, in x; x is refilled with k + 4 and k + 5
+    auto step = [&](Step& x, int k) {
+        const bool good[2] = {x.id[0] < pool, x.id[1] < pool};
+        const int tok = (s.first + k) * kBlockSize;
+        const bool tail = !good[0] || !good[1] || tok > s.L - 2 * kBlockSize;
+        float sc[8];
+        {
+            const f32x4 s0 = scores<G>(x.t[0], op), s1 = scores<G>(x.t[1], op);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                live[e] = good && tok + e < s.L;
-                sc[e] = live[e] ? sc[e] : -INFINITY;
-                vscale[e] = live[e] ? vscale[e] : 1.f;   // (an unused slot may hold a NaN scale)
+                sc[e] = s0[e];
+                sc[4 + e] = s1[e];
             }
         }
-        const float bm = apex::rows_max4(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])));
+        // a tile's registers are refilled as soon as they are read (in place: the
+        // barrier keeps the scheduler from issuing the loads above the reads)
+        __builtin_amdgcn_sched_barrier(0);
+        __amdgpu_buffer_rsrc_t refill[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            x.id[i] = x.next[i];
+            refill[i] = slab(x.id[i]);
+            load_keys(x.t[i], refill[i], lane);
+            x.next[i] = id_at(k + 8 + i);
+        }
+        bool live[8];
+        if (tail) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                live[e] = good[e >> 2] && tok + (e >> 2) * kBlockSize + 4 * q + (e & 3) < s.L;
+                sc[e] = live[e] ? sc[e] : -INFINITY;
+            }
+        }
+        float bm = sc[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) bm = fmaxf(bm, sc[e]);
+        bm = apex::rows_max4(bm);
         const float m = fmaxf(st.m, bm * p.scale_log2);
         const float ms = m == -INFINITY ? 0.f : m;   // no token so far
         const float alpha = apex::exp2_fast(st.m - ms);
-        float w[4];
+        float w[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = apex::exp2_fast(fmaf(sc[e], p.scale_log2, -ms));
+        for (int e = 0; e < 8; ++e) w[e] = apex::exp2_fast(fmaf(sc[e], p.scale_log2, -ms));
         if (tail) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = live[e] ? w[e] : 0.f;   // (a scale of 0 makes -inf a NaN)
+            for (int e = 0; e < 8; ++e) w[e] = live[e] ? w[e] : 0.f;   // (a scale of 0 makes -inf a NaN)
         }
-        st.l = fmaf(st.l, alpha, (w[0] + w[1]) + (w[2] + w[3]));
+        st.l = fmaf(st.l, alpha, ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7])));
         st.m = m;
         if (alpha != 1.f) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) st.acc[j] *= alpha;
         }
-        // weights as operand words
-        u32x4 hi, lo;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const unsigned u = __float_as_uint(w[e]);
-            if (G < 8) {
-                const unsigned part = __float_as_uint(w[e] - __uint_as_float(u & low_part));
-                hi[e] = __builtin_amdgcn_perm(0u, part, place);
-            } else {
-                hi[e] = __builtin_amdgcn_perm(0u, u, place);
-                lo[e] = __builtin_amdgcn_perm(0u, __float_as_uint(w[e] - __uint_as_float(u & 0xffff0000u)), place);
+        for (int i = 0; i < 2; ++i) {
+            // weights and values as operand words
+            u32x4 hi, lo, a[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float we = w[4 * i + e];
+                const unsigned u = __float_as_uint(we);
+                if (G < 8) {
+                    const unsigned part = __float_as_uint(we - __uint_as_float(u & low_part));
+                    hi[e] = __builtin_amdgcn_perm(0u, part, place);
+                } else {
+                    hi[e] = __builtin_amdgcn_perm(0u, u, place);
+                    lo[e] = __builtin_amdgcn_perm(0u, __float_as_uint(we - __uint_as_float(u & 0xffff0000u)), place);
+                }
             }
-        }
-        u32x4 a[4];
+            const unsigned vs = x.t[i].vs;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            a[0][e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[e], vscale[e], 0));
-            a[1][e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[e], vscale[e], 1));
-            a[2][e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[e], vscale[e], 2));
-            a[3][e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v[e], vscale[e], 3));
-        }
-        // the tile is consumed
-        __builtin_amdgcn_sched_barrier(0);
-        load(t, id);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            st.acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[j]),
-                                                                __builtin_bit_cast(bf16x8, hi), st.acc[j], 0, 0, 0);
-        if (G == 8) {
+            for (int e = 0; e < 4; ++e) {
+                float scale = __uint_as_float((e == 0 ? vs << 23 : e == 1 ? vs << 15 : e == 2 ? vs << 7 : vs >> 1) & 0x7f800000u);
+                if (tail) scale = live[4 * i + e] ? scale : 1.f;   // (an unused slot may hold a NaN scale)
+                const unsigned v = x.t[i].v[e];
+                a[0][e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, scale, 0));
+                a[1][e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, scale, 1));
+                a[2][e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, scale, 2));
+                a[3][e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v, scale, 3));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load_values(x.t[i], refill[i], lane);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 st.acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[j]),
-                                                                    __builtin_bit_cast(bf16x8, lo), st.acc[j], 0, 0, 0);
+                                                                    __builtin_bit_cast(bf16x8, hi), st.acc[j], 0, 0, 0);
+            if (G == 8) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    st.acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                        __builtin_bit_cast(bf16x8, a[j]), __builtin_bit_cast(bf16x8, lo), st.acc[j], 0, 0, 0);
+            }
         }
     };
-    for (int k = 0; k < s.n; k += kDepth) {
-#pragma unroll
-        for (int i = 0; i < kDepth; ++i)
-            if (k + i < s.n) block(tile[i], k + i, id[i], next[i]);
+    // pairs of steps, then an odd last one: straight code between the loads of
+    // a step and its waits
+    int k = 0;
+    for (; k + 2 < s.n; k += 4) {
+        step(x[0], k);
+        step(x[1], k + 2);
     }
+    if (k < s.n) step(x[0], k);
     st.l = apex::rows_sum4(st.l);
 }
 
-// A wave's state into LDS, [head][dim], to be merged with the other waves'.
+// A wave's state into LDS: sums [head][dim], maxima and sums of weights.
 template <int G>
-__device__ inline void store_state(State& st, int wave, int lane, float (*s_acc)[kStageFloats], float (*s_m)[G],
-                                   float (*s_l)[G])
+struct Shared {
+    __attribute__((aligned(16))) float acc[kWaves][G * kHeadDim];
+    float m[kWaves][G];
+    float l[kWaves][G];
+    int last;
+};
+
+template <int G>
+__device__ inline void store_state(State& st, int wave, int lane, Shared<G>& sh)
 {
     const int col = lane & 15, q = lane >> 4;
     if (G < 8) {
@@ -425,24 +575,87 @@ __device__ inline void store_state(State& st, int wave, int lane, float (*s_acc)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s_acc[wave][head * kHeadDim + 8 * (4 * q + i) + 2 * j + parity] = st.acc[j][i];
+            for (int j = 0; j < 4; ++j) sh.acc[wave][head * kHeadDim + 8 * (4 * q + i) + 2 * j + parity] = st.acc[j][i];
     }
     if (col < G && q == 0) {
-        s_m[wave][col] = st.m;
-        s_l[wave][col] = st.l;
+        sh.m[wave][col] = st.m;
+        sh.l[wave][col] = st.l;
     }
 }
 
-// Rows of the pair's heads: zeros and -inf where there was no token; NaNs stay.
+// N consecutive elements of a head's row: numerators and denominator relative
+// to 2^M.
+template <int N>
+struct Row {
+    float M, den;
+    float num[N];
+};
+
+template <int N>
+__device__ inline void clear(Row<N>& r)
+{
+    r.M = -INFINITY;
+    r.den = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.num[i] = 0.f;
+}
+
+// Rescales r to the running max of C more (max, sum) pairs, the first n of them
+// given, and adds their sums; f gets their factors.
+template <int N, int C>
+__device__ inline void join_sums(const float (&m)[C], const float (&l)[C], int n, Row<N>& r, float (&f)[C])
+{
+    float M = r.M;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        f[j] = j < n ? m[j] : -INFINITY;
+        M = fmaxf(M, f[j]);
+    }
+    const float Ms = M == -INFINITY ? 0.f : M;
+    const float f0 = apex::exp2_fast(r.M - Ms);
+    r.den *= f0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.num[i] *= f0;
+    r.M = M;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        f[j] = apex::exp2_fast(f[j] - Ms);
+        if (j < n) r.den = fmaf(f[j], l[j], r.den);
+    }
+}
+
+// The waves' states of head h at dims [dim, dim + N), joined.
+template <int G, int N>
+__device__ inline void join_waves(const Shared<G>& sh, int h, int dim, Row<N>& r)
+{
+    float m[kWaves], l[kWaves], f[kWaves];
+#pragma unroll
+    for (int j = 0; j < kWaves; ++j) {
+        m[j] = sh.m[j][h];
+        l[j] = sh.l[j][h];
+    }
+    clear(r);
+    join_sums<N, kWaves>(m, l, kWaves, r, f);
+#pragma unroll
+    for (int j = 0; j < kWaves; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) r.num[i] = fmaf(f[j], sh.acc[j][h * kHeadDim + dim + i], r.num[i]);
+}
+
+// The result's elements: zeros and -inf where there was no token; NaNs stay.
 // The cache can hold 65536 (65504 rounded up), whose half would be infinite: a
 // larger result than 65504 becomes that.
 template <int N>
-__device__ inline void emit_row(const AttnParams& p, int b, int head, int dim, const RowState<N>& r)
+__device__ inline void emit_row(const Params& p, int b, int head, int dim, const Row<N>& r)
 {
     typename apex::vec_of<f16, N>::type o;
+    const float inv = 1.f / r.den;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float x = r.den == 0.f ? 0.f : r.num[i] / r.den;
+        // a quotient by the reciprocal, corrected once: within a rounding of the
+        // division's, which takes three times the instructions
+        const float y = r.num[i] * inv;
+        const float x = r.den == 0.f ? 0.f : fmaf(fmaf(-y, r.den, r.num[i]), inv, y);
         o[i] = (f16)(__builtin_fabsf(x) > 65504.f ? __builtin_copysignf(65504.f, x) : x);
     }
     *(typename apex::vec_of<f16, N>::type*)&p.out[((size_t)b * p.Hq + head) * kHeadDim + dim] = o;
@@ -450,61 +663,145 @@ __device__ inline void emit_row(const AttnParams& p, int b, int head, int dim, c
         p.lse[(size_t)b * p.Hq + head] = r.den == 0.f ? -INFINITY : (r.M + __log2f(r.den)) * 0.69314718055994531f;
 }
 
-// Walks the work group's segments: f(b, g, L, nb, blk, take, vf) for each.
-template <typename F>
-__device__ inline void for_segments(const Kv4Params& p, int B, int Hkv, unsigned K, const Plan& plan, F f)
+// Partials of a split pair, written and read device-coherently: contributor c
+// (work group wf + c) has slot 2 (wf + c), the first one slot 2 wf + 1 (a work
+// group has at most two: the end of one pair, the start of another).
+__device__ inline int64_t partial_slot(int w, int wf) { return 2 * (int64_t)w + (w == wf); }
+
+template <int G>
+__device__ inline __amdgpu_buffer_rsrc_t partial_sums(const Params& p, int64_t slot, int n)
 {
-    int b = plan.b, g = plan.g, blk = plan.blk, L = plan.L;
-    unsigned vf = plan.vf;
-    while (vf + (unsigned)blk < plan.v1) {
-        const int nb = (int)blocks(L);
-        const int take = (int)min((unsigned)(nb - blk), plan.v1 - (vf + (unsigned)blk));
-        f(b, g, L, nb, blk, take, vf);
-        if (blk + take < nb) return;
-        vf += (unsigned)nb + K;
-        blk = 0;
-        if (++g == Hkv) {
-            g = 0;
-            do {
-                if (++b >= B) return;
-                L = uniform(cut_len(p, p.lens[b]));
-            } while (L <= 0);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)apex::uniform_ptr(p.pacc + slot * (G * kHeadDim)), (short)0,
+                                             n * 2 * G * kHeadDim * 4, apex::kRawBufferWord3);
+}
+
+template <int G>
+__device__ inline __amdgpu_buffer_rsrc_t partial_maxima(const Params& p, int64_t slot, int n)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((void*)apex::uniform_ptr(p.pml + slot * (G * 2)), (short)0, n * 2 * G * 8,
+                                             apex::kRawBufferWord3);
+}
+
+template <int G, int N>
+__device__ inline void store_partial(const Params& p, int64_t slot, int e0, int h, bool first, const Row<N>& r)
+{
+    const auto acc = partial_sums<G>(p, slot, 1);
+    if constexpr (N == 1)
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(r.num[0]), acc, e0 * 4, 0, apex::kCoherent);
+    else
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(r.num[0]), __float_as_uint(r.num[1])}, acc, e0 * 4, 0,
+                                              apex::kCoherent);
+    if (first) {
+        const u32x2 v = {__float_as_uint(r.M), __float_as_uint(r.den)};
+        __builtin_amdgcn_raw_buffer_store_b64(v, partial_maxima<G>(p, slot, 1), h * 8, 0, apex::kCoherent);
+    }
+}
+
+// Contributors [c0, c1) of a pair joined into this wave's state in LDS.  A lane
+// owns 2 G consecutive elements of the pair's rows and asks for kRows partials
+// at once: what a combine takes is round trips.
+template <int G>
+__device__ inline void join_partials(const Params& p, int wf, int c0, int c1, int wave, int lane, Shared<G>& sh)
+{
+    constexpr int N = 2 * G, kRows = 8, kVecs = G == 1 ? 1 : N / 4, kPer = N / kVecs;
+    typedef typename apex::vec_of<unsigned, kPer>::type word;
+    const int h = lane * N / kHeadDim, dim = lane * N % kHeadDim;
+    Row<N> r;
+    clear(r);
+    for (; c0 < c1; c0 += kRows) {
+        const int n = min(kRows, c1 - c0);
+        const auto acc = partial_sums<G>(p, 2 * (int64_t)(wf + c0), n), ml = partial_maxima<G>(p, 2 * (int64_t)(wf + c0), n);
+        float m[kRows], l[kRows], f[kRows];
+        word a[kRows][kVecs];
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {   // (reads past n give zeros)
+            const int slot = 2 * j + (j == 0 && c0 == 0);
+            const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(ml, h * 8 + slot * (G * 8), 0, apex::kCoherent);
+            m[j] = __uint_as_float(v[0]);
+            l[j] = __uint_as_float(v[1]);
+#pragma unroll
+            for (int k = 0; k < kVecs; ++k) {
+                const int off = lane * N * 4 + k * 16 + slot * (G * kHeadDim * 4);
+                if constexpr (G == 1)
+                    a[j][k] = __builtin_amdgcn_raw_buffer_load_b64(acc, off, 0, apex::kCoherent);
+                else
+                    a[j][k] = __builtin_amdgcn_raw_buffer_load_b128(acc, off, 0, apex::kCoherent);
+            }
         }
+        join_sums<N, kRows>(m, l, n, r, f);
+#pragma unroll
+        for (int j = 0; j < kRows; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) r.num[i] = fmaf(f[j], __uint_as_float(a[j][i / kPer][i % kPer]), r.num[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) sh.acc[wave][lane * N + i] = r.num[i];
+    if (dim == 0) {
+        sh.m[wave][h] = r.M;
+        sh.l[wave][h] = r.den;
     }
 }
 
 template <int G>
-__global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnParams p, Kv4Params kp)
+__global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
 {
-    __shared__ __align__(16) float s_acc[kWaves][kStageFloats];
-    __shared__ float s_m[kWaves][G];
-    __shared__ float s_l[kWaves][G];
-    __shared__ int s_last;
+    __shared__ Shared<G> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const unsigned w = blockIdx.x;
-    const Plan plan = make_plan(kp, p.B, p.Hkv, kPairCost, w, lane);
-    constexpr int N = apex::kEmitElems<G>;
-    const int h = tid * N / kHeadDim, dim = tid * N % kHeadDim;
-    const bool emits = G >= 2 || tid < kHeadDim;
+    const int w = (int)blockIdx.x;
+    Plan plan = make_plan<true>(p, kPairCost, (unsigned)w, lane);
 
-    for_segments(kp, p.B, p.Hkv, kPairCost, plan, [&](int b, int g, int L, int nb, int blk, int take, unsigned vf) {
+    if (plan.way == kWhole) {
+        // every wave takes whole pairs, and writes their rows itself
+        constexpr int N = 2 * G;
+        const int h = lane * N / kHeadDim, dim = lane * N % kHeadDim;
+        const int pairs = p.B * p.Hkv;
+        for (int i = wave * p.workers + w; i < pairs; i += kWaves * p.workers) {
+            const int b = uniform((int)((unsigned)i / (unsigned)p.Hkv)), g = i - b * p.Hkv;
+            const int L = uniform(context(p, b));
+            Row<N> r;
+            clear(r);
+            if (L > 0) {
+                State st;
+                attend<G>(p, b, g, wave_span(p, b, g, L, 0, (int)blocks(L), 0, 1), lane, st);
+                store_state<G>(st, wave, lane, sh);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                r.M = sh.m[wave][h];
+                r.den = sh.l[wave][h];
+#pragma unroll
+                for (int e = 0; e < N; ++e) r.num[e] = sh.acc[wave][lane * N + e];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            }
+            emit_row<N>(p, b, g * G + h, dim, r);
+        }
+        return;
+    }
+
+    constexpr int N = G == 8 ? 2 : 1;
+    const int h = tid * N / kHeadDim, dim = tid * N % kHeadDim;
+    const bool emits = h < G;
+    bool more = plan.take > 0;
+    while (more) {
+        const int b = plan.b, g = plan.g;
+        const int nb = (int)blocks(plan.L);
         {
-            QueryOperand<G> op;
-            load_query<G>(p, kp.q_sign, b, g, lane, op);
             State st;
-            attend<G>(kp, p.Hkv, wave_span(kp, b, g, L, blk, blk + take, wave), op, lane, st);
-            store_state<G>(st, wave, lane, s_acc, s_m, s_l);
+            attend<G>(p, b, g, wave_span(p, b, g, plan.L, plan.blk, plan.blk + plan.take, wave, kWaves), lane, st);
+            store_state<G>(st, wave, lane, sh);
         }
         __syncthreads();
         // the pair's first and last work groups
-        const int wf = blk == 0 ? (int)w : uniform((int)plan.line.owner(vf));
-        const int wl = blk + take == nb ? (int)w : uniform((int)plan.line.owner(vf + (unsigned)nb - 1));
+        int wf = plan.first, wl = plan.last;
+        if (plan.way == kLine) {
+            wf = plan.blk == 0 ? w : uniform((int)plan.line.owner(plan.vf));
+            wl = plan.blk + plan.take == nb ? w : uniform((int)plan.line.owner(plan.vf + (unsigned)nb - 1));
+        }
         if (emits) {
-            const RowState<N> r = apex::merge_waves<G, N>(s_acc, s_m, s_l, h, dim);
+            Row<N> r;
+            join_waves<G, N>(sh, h, dim, r);
             if (wf == wl)
                 emit_row<N>(p, b, g * G + h, dim, r);
             else
-                apex::store_partial<G, N>(p, apex::partial_slot(w, wf), tid * N, h, dim == 0, r);
+                store_partial<G, N>(p, partial_slot(w, wf), tid * N, h, dim == 0, r);
         }
         if (wf != wl) {
             // the partials are written with device-coherent stores, complete
@@ -517,29 +814,30 @@ __global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnParams p, K
                 const int old = __hip_atomic_fetch_add(cnt, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 const int last = old == wl - wf;
                 if (last) __hip_atomic_store(cnt, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                s_last = last;
+                sh.last = last;
             }
             __syncthreads();
-            if (s_last) {
+            if (sh.last) {
                 const int nc = wl - wf + 1, per = (nc + kWaves - 1) / kWaves;
-                const int c0 = wave * per;
-                apex::combine_wave<G>(p, wf, c0, c0 + per < nc ? c0 + per : nc, wave, lane, s_acc, s_m, s_l);
+                join_partials<G>(p, wf, wave * per, min(nc, wave * per + per), wave, lane, sh);
                 __syncthreads();
-                if (emits) emit_row<N>(p, b, g * G + h, dim, apex::merge_waves<G, N>(s_acc, s_m, s_l, h, dim));
+                if (emits) {
+                    Row<N> r;
+                    join_waves<G, N>(sh, h, dim, r);
+                    emit_row<N>(p, b, g * G + h, dim, r);
+                }
             }
         }
-        __syncthreads();
-    });
+        more = plan.way == kLine && next_segment(p, kPairCost, plan);
+        if (more) __syncthreads();
+    }
 
     if (plan.empty_rows) {
-        for (int b = (int)w; b < p.B; b += (int)gridDim.x) {
-            if (cut_len(kp, kp.lens[b]) > 0) continue;
-            RowState<1> r;
-            r.M = 0.f;
-            r.den = 0.f;
-            r.num = 0.f;
-            for (int i = tid; i < p.Hq * kHeadDim; i += kAttnThreads)
-                emit_row<1>(p, b, i / kHeadDim, i % kHeadDim, r);
+        for (int b = w; b < p.B; b += (int)gridDim.x) {
+            if (context(p, b) > 0) continue;
+            Row<1> r;
+            clear(r);
+            for (int i = tid; i < p.Hq * kHeadDim; i += kThreads) emit_row<1>(p, b, i / kHeadDim, i % kHeadDim, r);
         }
     }
 }
@@ -547,68 +845,97 @@ __global__ __launch_bounds__(kAttnThreads) void attention_kernel(AttnParams p, K
 // --- accumulated weights ----------------------------------------------------------
 
 // Every block is on its own: its K codes and scales, the scores, the weights of
-// 16 tokens added up over the heads, 64 bytes read and written.
-template <int G>
-__global__ __launch_bounds__(kAttnThreads) void weights_kernel(AttnParams p, Kv4Params kp)
-{
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    const int col = lane & 15, q = lane >> 4;
-    const Plan plan = make_plan(kp, p.B, p.Hkv, kPairCost, blockIdx.x, lane);
-    const uint64_t step = (uint64_t)p.Hkv * kSlabBytes;
+// 16 tokens added up over the heads, 64 bytes read and written by the four lanes
+// of column 0.  Two blocks a step and two steps in flight, as in the attention.
+constexpr int kWeightThreads = 256;
+constexpr int kWeightGroupsPerCu = 4;
+constexpr unsigned kWeightPairCost = 8;
 
-    for_segments(kp, p.B, p.Hkv, kPairCost, plan, [&](int b, int g, int L, int, int blk, int take, unsigned) {
-        QueryOperand<G> op;
-        load_query<G>(p, kp.q_sign, b, g, lane, op);
-        const int head = G == 8 ? col & 7 : (col & 3) & (G - 1);
-        const float lse2 = kp.lse_in[(size_t)b * p.Hq + (size_t)g * G + head] * 1.4426950408889634f;
-        const Span s = wave_span(kp, b, g, L, blk, blk + take, wave);
-        for (int k = 0; k < s.n; ++k) {
-            const int id = uniform(s.bt[k]);
-            if (id < 0 || (int64_t)id >= kp.num_blocks) continue;
-            Tile t;
-            load_tile<false>(t, s.pair + (uint64_t)(uint32_t)id * step, kSlabBytes, lane);
-            const f32x4 sc = scores<G>(t, op);
-            f32x4 w;
+struct KeyTile {
+    Tile t;
+    f32x4 old;
+};
+
+template <int G>
+__device__ inline void accumulate(const Params& p, int b, int g, const Span& s, int lane)
+{
+    const int col = lane & 15, q = lane >> 4;
+    const uint64_t step_bytes = (uint64_t)p.Hkv * kSlabBytes, step_weights = (uint64_t)p.Hkv * kBlockSize;
+    float* const to = apex::uniform_ptr(p.weights + (size_t)uniform(g) * kBlockSize);
+    // column 0 reads and writes, the others lie past the extent
+    const int woff = col == 0 ? q * 16 : 1 << 20;
+    auto id_at = [&](int i) -> unsigned {
+        const unsigned id = *(const __attribute__((address_space(4))) uint32_t*)(s.bt + (i < s.n ? i : 0));
+        return i < s.n ? id : 0xffffffffu;
+    };
+    auto slots = [&](unsigned id) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)apex::uniform_ptr(to + id * step_weights), (short)0,
+                                                 id < p.num_blocks ? kBlockSize * 4 : 0, apex::kRawBufferWord3);
+    };
+    auto load = [&](KeyTile& x, unsigned id) {
+        load_keys(x.t, slab_resource(s.pair + id * step_bytes, id < p.num_blocks ? kSlabBytes : 0), lane);
+        x.old = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(slots(id), woff, 0, 0));
+    };
+    constexpr int kAhead = 4;
+    KeyTile x[kAhead];
+    unsigned id[kAhead], next[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        id[i] = id_at(i);
+        load(x[i], id[i]);
+        next[i] = id_at(kAhead + i);
+    }
+    QueryOperand<G> op;
+    load_query<G>(p, b, g, lane, op);
+    const int head = G == 8 ? col & 7 : (col & 3) & (G - 1);
+    const float lse2 = p.lse_in[(size_t)b * p.Hq + (size_t)g * G + head] * 1.4426950408889634f;
+    // (a last round's surplus blocks have no extent: they read zeros and write nothing)
+    for (int k = 0; k < s.n; k += kAhead) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            f32x4 w = scores<G>(x[i].t, op);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                float x = apex::exp2_fast(fmaf(sc[e], kp.scale_log2, -lse2));
-                if (G >= 2) x = add_rotated<0xb1>(x);      // lanes 1, 0, 3, 2
-                if (G >= 4) x = add_rotated<0x4e>(x);      // lanes 2, 3, 0, 1
-                if (G == 8) x = add_rotated<kRor4>(x);
-                w[e] = x;
+                w[e] = apex::exp2_fast(fmaf(w[e], p.scale_log2, -lse2));
+                if (G >= 2) w[e] = add_rotated<0xb1>(w[e]);      // lanes 1, 0, 3, 2
+                if (G >= 4) w[e] = add_rotated<0x4e>(w[e]);      // lanes 2, 3, 0, 1
+                if (G == 8) w[e] = add_rotated<kRor4>(w[e]);
             }
-            if (col == 0) {
-                const int tok = (s.first + k) * kBlockSize + 4 * q;
-                f32x4* to = (f32x4*)(kp.weights + ((uint64_t)(uint32_t)id * p.Hkv + g) * kBlockSize + 4 * q);
-                f32x4 old = *to;
+            const int tok = (s.first + k + i) * kBlockSize + 4 * q;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) old[e] = tok + e < s.L ? old[e] + w[e] : old[e];
-                *to = old;
-            }
+            for (int e = 0; e < 4; ++e) w[e] = tok + e < s.L ? x[i].old[e] + w[e] : x[i].old[e];
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, w), slots(id[i]), woff, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            id[i] = next[i];
+            load(x[i], id[i]);
+            next[i] = id_at(k + 2 * kAhead + i);
         }
-    });
+    }
+}
+
+template <int G>
+__global__ __launch_bounds__(kWeightThreads, 4) void weights_kernel(Params p)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    Plan plan = make_plan<false>(p, kWeightPairCost, blockIdx.x, lane);
+    bool more = plan.take > 0;
+    while (more) {
+        const Span s = wave_span(p, plan.b, plan.g, plan.L, plan.blk, plan.blk + plan.take, wave, kWeightThreads / 64);
+        if (s.n > 0) accumulate<G>(p, plan.b, plan.g, s, lane);
+        more = next_segment(p, kWeightPairCost, plan);
+    }
 }
 
 // --- host -------------------------------------------------------------------------
 
-constexpr int kGroupsPerCu = 4;
-
-int workers(int64_t* out)
-{
-    int cus = 0;
-    const int rc = kv4::compute_units(&cus);
-    *out = (int64_t)cus * kGroupsPerCu;
-    return rc;
-}
-
 size_t counter_bytes(int B, int Hkv) { return kv4::align_up((size_t)B * Hkv * sizeof(int32_t), 256); }
 
-size_t acc_bytes(int64_t workers, int G)
+size_t acc_bytes(int workers, int G)
 {
     return kv4::align_up(sizeof(float) * 2 * (size_t)workers * G * kHeadDim, 256);
 }
 
-size_t partial_bytes(int64_t workers, int G)
+size_t partial_bytes(int workers, int G)
 {
     return acc_bytes(workers, G) + kv4::align_up(sizeof(float) * 4 * (size_t)workers * G, 256);
 }
@@ -624,35 +951,34 @@ void with_group(int G, F f)
     }
 }
 
-int check_pointers(const void* q, const void* cache, const void* bt, const void* lens, const void* more, const char* name,
-                   size_t align)
+int check_pointers(const void* q, const void* cache, const void* bt, const void* lens, const void* more, const char* name)
 {
     if (!q || !cache || !bt || !lens || !more) return fail(APEX_ERR_INVALID_ARG, "a tensor pointer is NULL");
     if (!kv4::aligned(q, 16) || !kv4::aligned(cache, 16))
         return fail(APEX_ERR_INVALID_ARG, "q and kv_cache must be 16-byte aligned");
     if (!kv4::aligned(bt, 4) || !kv4::aligned(lens, 4))
         return fail(APEX_ERR_INVALID_ARG, "block_table and context_lens must be 4-byte aligned");
-    if (!kv4::aligned(more, align)) return fail(APEX_ERR_INVALID_ARG, "%s must be 16-byte aligned", name);
+    if (!kv4::aligned(more, 16)) return fail(APEX_ERR_INVALID_ARG, "%s must be 16-byte aligned", name);
     return APEX_OK;
 }
 
-void fill(AttnParams& p, Kv4Params& kp, const void* q, const void* cache, const int32_t* bt, int64_t stride,
-          const int32_t* lens, int B, int Hq, int Hkv, int64_t num_blocks, float scale, int64_t workers)
+Params fill(const void* q, const void* cache, const int32_t* bt, int64_t stride, const int32_t* lens, int B, int Hq,
+            int Hkv, int64_t num_blocks, float scale, int workers)
 {
-    p = AttnParams();
+    Params p = Params();
     p.q = (const f16*)q;
+    p.cache = (const char*)cache;
+    p.bt = bt;
+    p.lens = lens;
+    p.num_blocks = (unsigned)num_blocks;
+    p.stride = (int)stride;
     p.B = B;
     p.Hq = Hq;
     p.Hkv = Hkv;
-    kp = Kv4Params();
-    kp.cache = (const char*)cache;
-    kp.bt = bt;
-    kp.lens = lens;
-    kp.num_blocks = num_blocks;
-    kp.stride = (int)stride;
-    kp.workers = (int)workers;
-    kp.scale_log2 = __builtin_fabsf(scale) * 1.4426950408889634f;
-    kp.q_sign = __builtin_signbit(scale) ? 0x8000u : 0u;
+    p.workers = workers;
+    p.scale_log2 = __builtin_fabsf(scale) * 1.4426950408889634f;
+    p.q_sign = __builtin_signbit(scale) ? 0x8000u : 0u;
+    return p;
 }
 
 }  // namespace
@@ -672,9 +998,10 @@ size_t apex_kv4_attention_counter_bytes(int B, int Hkv)
 size_t apex_kv4_attention_workspace_bytes(int B, int Hq, int Hkv)
 {
     apex::clear_error();
-    int64_t n = 0;
-    if (kv4::check_batch(B, Hq, Hkv, kHeadDim, kBlockSize, 0, 0) != APEX_OK || workers(&n) != APEX_OK) return 0;
-    return counter_bytes(B, Hkv) + partial_bytes(n, Hq / Hkv);
+    int cus = 0;
+    if (kv4::check_batch(B, Hq, Hkv, kHeadDim, kBlockSize, 0, 0) != APEX_OK || kv4::compute_units(&cus) != APEX_OK)
+        return 0;
+    return counter_bytes(B, Hkv) + partial_bytes(cus, Hq / Hkv);
 }
 
 int apex_kv4_attention(const void* q, const void* kv_cache, const int32_t* block_table, int64_t block_table_stride,
@@ -685,7 +1012,7 @@ int apex_kv4_attention(const void* q, const void* kv_cache, const int32_t* block
     apex::clear_error();
     int rc = kv4::check_batch(B, Hq, Hkv, d, block_size, num_blocks, block_table_stride);
     if (rc != APEX_OK || B == 0) return rc;
-    rc = check_pointers(q, kv_cache, block_table, context_lens, out, "out", 16);
+    rc = check_pointers(q, kv_cache, block_table, context_lens, out, "out");
     if (rc != APEX_OK) return rc;
     if (!kv4::aligned(lse_out, 4)) return fail(APEX_ERR_INVALID_ARG, "lse_out must be 4-byte aligned");
     const size_t qo = (size_t)B * Hq * d * 2;
@@ -699,11 +1026,11 @@ int apex_kv4_attention(const void* q, const void* kv_cache, const int32_t* block
     if ((rc = kv4::check_disjoint(in[4], in, 4)) != APEX_OK || (rc = kv4::check_disjoint(in[5], in, 5)) != APEX_OK ||
         (rc = kv4::check_disjoint(in[6], in, 6)) != APEX_OK)
         return rc;
-    int64_t n = 0;
-    rc = workers(&n);
+    int cus = 0;
+    rc = kv4::compute_units(&cus);
     if (rc != APEX_OK) return rc;
     const int G = Hq / Hkv;
-    const size_t cb = counter_bytes(B, Hkv), pb = partial_bytes(n, G);
+    const size_t cb = counter_bytes(B, Hkv), pb = partial_bytes(cus, G);
     void *counters = workspace, *partials = (char*)workspace + cb;
     if (workspace) {
         rc = kv4::check_workspace(workspace, workspace_bytes, cb + pb);
@@ -712,16 +1039,14 @@ int apex_kv4_attention(const void* q, const void* kv_cache, const int32_t* block
         if (rc == APEX_OK) rc = kv4::library_buffer(kv4::kPartials, pb, (hipStream_t)stream, &partials);
     }
     if (rc != APEX_OK) return rc;
-    AttnParams p;
-    Kv4Params kp;
-    fill(p, kp, q, kv_cache, block_table, block_table_stride, context_lens, B, Hq, Hkv, num_blocks, scale, n);
+    Params p = fill(q, kv_cache, block_table, block_table_stride, context_lens, B, Hq, Hkv, num_blocks, scale, cus);
     p.out = (f16*)out;
     p.lse = lse_out;
     p.counters = (int32_t*)counters;
     p.pacc = (float*)partials;
-    p.pml = (float*)((char*)partials + acc_bytes(n, G));
+    p.pml = (float*)((char*)partials + acc_bytes(cus, G));
     with_group(G, [&](auto g) {
-        attention_kernel<decltype(g)::value><<<(unsigned)n, kAttnThreads, 0, (hipStream_t)stream>>>(p, kp);
+        attention_kernel<decltype(g)::value><<<(unsigned)cus, kThreads, 0, (hipStream_t)stream>>>(p);
     });
     return kv4::launched("kv4 attention");
 }
@@ -734,7 +1059,7 @@ int apex_kv4_accumulate_weights(const void* q, const void* kv_cache, const int32
     apex::clear_error();
     int rc = kv4::check_batch(B, Hq, Hkv, d, block_size, num_blocks, block_table_stride);
     if (rc != APEX_OK || B == 0) return rc;
-    rc = check_pointers(q, kv_cache, block_table, context_lens, weights, "weights", 16);
+    rc = check_pointers(q, kv_cache, block_table, context_lens, weights, "weights");
     if (rc != APEX_OK) return rc;
     if (!lse) return fail(APEX_ERR_INVALID_ARG, "a tensor pointer is NULL");
     if (!kv4::aligned(lse, 4)) return fail(APEX_ERR_INVALID_ARG, "lse must be 4-byte aligned");
@@ -746,16 +1071,15 @@ int apex_kv4_accumulate_weights(const void* q, const void* kv_cache, const int32
                               {"weights", weights, kv4::slot_bytes(Hkv, num_blocks)}};
     rc = kv4::check_disjoint(in[5], in, 5);
     if (rc != APEX_OK) return rc;
-    int64_t n = 0;
-    rc = workers(&n);
+    int cus = 0;
+    rc = kv4::compute_units(&cus);
     if (rc != APEX_OK) return rc;
-    AttnParams p;
-    Kv4Params kp;
-    fill(p, kp, q, kv_cache, block_table, block_table_stride, context_lens, B, Hq, Hkv, num_blocks, scale, n);
-    kp.lse_in = lse;
-    kp.weights = weights;
+    const int n = cus * kWeightGroupsPerCu;
+    Params p = fill(q, kv_cache, block_table, block_table_stride, context_lens, B, Hq, Hkv, num_blocks, scale, n);
+    p.lse_in = lse;
+    p.weights = weights;
     with_group(Hq / Hkv, [&](auto g) {
-        weights_kernel<decltype(g)::value><<<(unsigned)n, kAttnThreads, 0, (hipStream_t)stream>>>(p, kp);
+        weights_kernel<decltype(g)::value><<<(unsigned)n, kWeightThreads, 0, (hipStream_t)stream>>>(p);
     });
     return kv4::launched("kv4 weights");
 }
