@@ -146,23 +146,32 @@ __device__ inline unsigned part_blocks(unsigned nb, unsigned least)
     return max(t, least);
 }
 
-template <bool kAttention>
-__device__ inline Plan make_plan(const Params& p, unsigned K, unsigned w, int lane)
+// Up to 64 requests (kFew) a lane holds one, and the plan reads the lengths once.
+template <bool kAttention, bool kFew>
+__device__ inline Plan plan_of(const Params& p, unsigned hk, unsigned K, unsigned w, int lane)
 {
-    const int R = (p.B + 63) / 64;
+    const int R = kFew ? 1 : (p.B + 63) / 64;
     const int r0 = min(p.B, lane * R), r1 = min(p.B, r0 + R);
+    const int own = r0 < r1 ? context(p, r0) : 0;   // the lane's only request's length (kFew)
+    auto sum = [&](auto f) -> unsigned {            // of f(blocks) over the lane's requests
+        if (kFew) return f(blocks(own));
+        unsigned n = 0;
+        for (int b = r0; b < r1; ++b) n += f(blocks(context(p, b)));
+        return n;
+    };
+    auto length = [&](int b) -> int { return kFew ? apex::lane_value(own, b) : uniform(context(p, b)); };
     unsigned units = 0, count = 0, longest = 0;
-    for (int b = r0; b < r1; ++b) {
-        const unsigned nb = blocks(context(p, b));
+    sum([&](unsigned nb) -> unsigned {
         units += nb;
         count += nb > 0;
         longest = max(longest, nb);
-    }
-    const unsigned hk = (unsigned)p.Hkv;
+        return 0;
+    });
     const unsigned cost = units + K * count;
     const unsigned hi = (unsigned)apex::wave_incl_sum((int)cost), lo = hi - cost;
     const unsigned total = (unsigned)apex::lane_value((int)hi, 63);
-    const unsigned nonempty = (unsigned)apex::lane_value(apex::wave_incl_sum((int)count), 63);
+    const unsigned nonempty = kFew ? (unsigned)__popcll(__ballot(count > 0))
+                                   : (unsigned)apex::lane_value(apex::wave_incl_sum((int)count), 63);
     longest = (unsigned)apex::lane_value(apex::wave_incl_max((int)longest), 63);
     Plan r;
     r.way = kLine;
@@ -170,7 +179,6 @@ __device__ inline Plan make_plan(const Params& p, unsigned K, unsigned w, int la
     r.v1 = r.vf = 0;
     r.b = r.g = r.blk = r.L = r.take = r.first = r.last = 0;
     const unsigned V = total * hk, pairs = nonempty * hk, U = V - K * pairs, W = (unsigned)p.workers;
-    r.line.set(V, W);
     if (U == 0) return r;
     if (kAttention && pairs > W && longest <= kWholeBlocks) {
         r.way = kWhole;
@@ -181,12 +189,10 @@ __device__ inline Plan make_plan(const Params& p, unsigned K, unsigned w, int la
         const unsigned least = longest <= 2 * kMinPart ? longest : room > 0 ? (U + room - 1) / room : U;
         if (least <= kMaxPart) {
             // the parts of the requests before a lane's, then the request of part w
-            unsigned parts = 0;
-            for (int b = r0; b < r1; ++b) {
-                const unsigned nb = blocks(context(p, b));
+            const unsigned parts = sum([&](unsigned nb) -> unsigned {
                 const unsigned t = part_blocks(nb, least);
-                parts += (nb + t - 1) / t;
-            }
+                return (nb + t - 1) / t;
+            });
             r.way = kParts;
             const unsigned phi = (unsigned)apex::wave_incl_sum((int)parts), plo = phi - parts;
             const uint64_t hit = __ballot(plo * hk <= w && w < phi * hk);
@@ -196,7 +202,7 @@ __device__ inline Plan make_plan(const Params& p, unsigned K, unsigned w, int la
             unsigned nb, t, c;
             for (int b = ln * R;; ++b) {
                 r.b = b;
-                r.L = uniform(context(p, b));
+                r.L = length(b);
                 nb = blocks(r.L);
                 t = part_blocks(nb, least);
                 c = (nb + t - 1) / t;
@@ -214,6 +220,7 @@ __device__ inline Plan make_plan(const Params& p, unsigned K, unsigned w, int la
             return r;
         }
     }
+    r.line.set(V, W);
     const unsigned v0 = r.line.start(w);
     r.v1 = r.line.start(w + 1);
     if (v0 >= r.v1) return r;
@@ -223,7 +230,7 @@ __device__ inline Plan make_plan(const Params& p, unsigned K, unsigned w, int la
     unsigned nb;
     for (int b = ln * R;; ++b) {
         r.b = b;
-        r.L = uniform(context(p, b));
+        r.L = length(b);
         nb = blocks(r.L);
         const unsigned span = nb > 0 ? (nb + K) * hk : 0u;
         if (v0 < at + span) break;
@@ -237,15 +244,22 @@ __device__ inline Plan make_plan(const Params& p, unsigned K, unsigned w, int la
     return r;
 }
 
+template <bool kAttention>
+__device__ inline Plan make_plan(const Params& p, int heads, unsigned K, unsigned w, int lane)
+{
+    const unsigned hk = (unsigned)heads;
+    return p.B <= 64 ? plan_of<kAttention, true>(p, hk, K, w, lane) : plan_of<kAttention, false>(p, hk, K, w, lane);
+}
+
 // Moves a line's plan to the work group's next segment; false when it has none.
-__device__ inline bool next_segment(const Params& p, unsigned K, Plan& r)
+__device__ inline bool next_segment(const Params& p, int heads, unsigned K, Plan& r)
 {
     const unsigned nb = blocks(r.L);
     if ((unsigned)(r.blk + r.take) < nb) return false;   // the range ended inside the pair
     r.vf += nb + K;
     r.blk = 0;
     if (r.vf >= r.v1) return false;
-    if (++r.g == p.Hkv) {
+    if (++r.g == heads) {
         r.g = 0;
         do {
             if (++r.b >= p.B) return false;
@@ -327,11 +341,15 @@ __device__ inline __amdgpu_buffer_rsrc_t slab_resource(const char* slab, int byt
     return __builtin_amdgcn_make_buffer_rsrc((void*)apex::uniform_ptr(slab), (short)0, bytes, apex::kRawBufferWord3);
 }
 
+// K goes through the Infinity Cache: a step that accumulates its weights reads
+// it again.  (Attention and accumulation of four caches in turn, 32 requests of
+// 8192 tokens, G = 4: 80.7 us a cache, 89.3 with K read past it; the attention
+// alone is the same either way.)  V is read once and past it.
 __device__ inline void load_keys(Tile& t, __amdgpu_buffer_rsrc_t r, int lane)
 {
     const int c = lane & 15, q = lane >> 4;
-    t.k = __builtin_amdgcn_raw_buffer_load_b128(r, c * 64 + q * 16, 0, apex::kStreamingLoad);
-    t.ks = __builtin_amdgcn_raw_buffer_load_b8(r, kv4::kKScales + c * 4 + q, 0, apex::kStreamingLoad);
+    t.k = __builtin_amdgcn_raw_buffer_load_b128(r, c * 64 + q * 16, 0, 0);
+    t.ks = __builtin_amdgcn_raw_buffer_load_b8(r, kv4::kKScales + c * 4 + q, 0, 0);
 }
 
 __device__ inline void load_values(Tile& t, __amdgpu_buffer_rsrc_t r, int lane)
@@ -748,7 +766,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
     __shared__ Shared<G> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int w = (int)blockIdx.x;
-    Plan plan = make_plan<true>(p, kPairCost, (unsigned)w, lane);
+    Plan plan = make_plan<true>(p, p.Hkv, kPairCost, (unsigned)w, lane);
 
     if (plan.way == kWhole) {
         // every wave takes whole pairs, and writes their rows itself
@@ -828,7 +846,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
                 }
             }
         }
-        more = plan.way == kLine && next_segment(p, kPairCost, plan);
+        more = plan.way == kLine && next_segment(p, p.Hkv, kPairCost, plan);
         if (more) __syncthreads();
     }
 
@@ -844,85 +862,97 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
 
 // --- accumulated weights ----------------------------------------------------------
 
-// Every block is on its own: its K codes and scales, the scores, the weights of
-// 16 tokens added up over the heads, 64 bytes read and written by the four lanes
-// of column 0.  Two blocks a step and two steps in flight, as in the attention.
+// Every block is on its own: its K codes and scales, the scores, and 16 sums over
+// the heads.  A wave collects the sums of kChunk blocks in LDS and adds them to
+// the weights with one load and one store of all its lanes (four lanes to a
+// block): a load and a store for every block, by four lanes each, put a store
+// into the wait for every K tile, 37 us against 30 without the stores.
 constexpr int kWeightThreads = 256;
-constexpr int kWeightGroupsPerCu = 4;
-constexpr unsigned kWeightPairCost = 8;
-
-struct KeyTile {
-    Tile t;
-    f32x4 old;
-};
+constexpr int kWeightWaves = kWeightThreads / 64;
+constexpr int kWeightGroupsPerCu = 3;
+constexpr unsigned kWeightPairCost = 16;
+constexpr int kChunk = 16, kAhead = 4;   // blocks; K tiles on their way
 
 template <int G>
-__device__ inline void accumulate(const Params& p, int b, int g, const Span& s, int lane)
+__device__ inline void accumulate(const Params& p, int b, int g, const Span& s, int lane, float* sums)
 {
     const int col = lane & 15, q = lane >> 4;
-    const uint64_t step_bytes = (uint64_t)p.Hkv * kSlabBytes, step_weights = (uint64_t)p.Hkv * kBlockSize;
-    float* const to = apex::uniform_ptr(p.weights + (size_t)uniform(g) * kBlockSize);
-    // column 0 reads and writes, the others lie past the extent
-    const int woff = col == 0 ? q * 16 : 1 << 20;
+    const uint64_t step_bytes = (uint64_t)p.Hkv * kSlabBytes;
     auto id_at = [&](int i) -> unsigned {
         const unsigned id = *(const __attribute__((address_space(4))) uint32_t*)(s.bt + (i < s.n ? i : 0));
         return i < s.n ? id : 0xffffffffu;
     };
-    auto slots = [&](unsigned id) {
-        return __builtin_amdgcn_make_buffer_rsrc((void*)apex::uniform_ptr(to + id * step_weights), (short)0,
-                                                 id < p.num_blocks ? kBlockSize * 4 : 0, apex::kRawBufferWord3);
+    auto load = [&](Tile& t, unsigned id) {
+        load_keys(t, slab_resource(s.pair + id * step_bytes, id < p.num_blocks ? kSlabBytes : 0), lane);
     };
-    auto load = [&](KeyTile& x, unsigned id) {
-        load_keys(x.t, slab_resource(s.pair + id * step_bytes, id < p.num_blocks ? kSlabBytes : 0), lane);
-        x.old = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(slots(id), woff, 0, 0));
-    };
-    constexpr int kAhead = 4;
-    KeyTile x[kAhead];
-    unsigned id[kAhead], next[kAhead];
+    // the lane's block of a chunk and its four tokens there
+    const int own = lane >> 2, tok = 4 * (lane & 3);
+    auto own_id = [&](int k) -> unsigned { return k + own < s.n ? (unsigned)s.bt[k + own] : 0xffffffffu; };
+    unsigned lane_id = own_id(0);
+    Tile t[kAhead];
+    unsigned next[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-        id[i] = id_at(i);
-        load(x[i], id[i]);
+        load(t[i], id_at(i));
         next[i] = id_at(kAhead + i);
     }
     QueryOperand<G> op;
     load_query<G>(p, b, g, lane, op);
     const int head = G == 8 ? col & 7 : (col & 3) & (G - 1);
     const float lse2 = p.lse_in[(size_t)b * p.Hq + (size_t)g * G + head] * 1.4426950408889634f;
-    // (a last round's surplus blocks have no extent: they read zeros and write nothing)
-    for (int k = 0; k < s.n; k += kAhead) {
+    for (int k = 0; k < s.n; k += kChunk) {
+        const bool live = lane_id < p.num_blocks;
+        f32x4* const to = (f32x4*)(p.weights + ((uint64_t)(live ? lane_id : 0) * p.Hkv + g) * kBlockSize + tok);
+        f32x4 old = {0.f, 0.f, 0.f, 0.f};
+        if (live) old = *to;
+        lane_id = own_id(k + kChunk);
+        // (surplus blocks of the last rounds have no extent, and no lane adds their sums)
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            f32x4 w = scores<G>(x[i].t, op);
+        for (int j = 0; j < kChunk; j += kAhead) {
+            if (k + j >= s.n) break;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                w[e] = apex::exp2_fast(fmaf(w[e], p.scale_log2, -lse2));
-                if (G >= 2) w[e] = add_rotated<0xb1>(w[e]);      // lanes 1, 0, 3, 2
-                if (G >= 4) w[e] = add_rotated<0x4e>(w[e]);      // lanes 2, 3, 0, 1
-                if (G == 8) w[e] = add_rotated<kRor4>(w[e]);
+            for (int i = 0; i < kAhead; ++i) {
+                f32x4 w = scores<G>(t[i], op);
+                __builtin_amdgcn_sched_barrier(0);
+                load(t[i], next[i]);
+                next[i] = id_at(k + j + 2 * kAhead + i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    w[e] = apex::exp2_fast(fmaf(w[e], p.scale_log2, -lse2));
+                    if (G >= 2) w[e] = add_rotated<0xb1>(w[e]);      // lanes 1, 0, 3, 2
+                    if (G >= 4) w[e] = add_rotated<0x4e>(w[e]);      // lanes 2, 3, 0, 1
+                    if (G == 8) w[e] = add_rotated<kRor4>(w[e]);
+                }
+                if (col == 0) *(f32x4*)&sums[(j + i) * kBlockSize + 4 * q] = w;
             }
-            const int tok = (s.first + k + i) * kBlockSize + 4 * q;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const f32x4 w = *(const f32x4*)&sums[own * kBlockSize + tok];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (live) {
+            const int at = (s.first + k + own) * kBlockSize + tok;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = tok + e < s.L ? x[i].old[e] + w[e] : x[i].old[e];
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, w), slots(id[i]), woff, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-            id[i] = next[i];
-            load(x[i], id[i]);
-            next[i] = id_at(k + 2 * kAhead + i);
+            for (int e = 0; e < 4; ++e) old[e] = at + e < s.L ? old[e] + w[e] : old[e];
+            *to = old;
         }
     }
 }
 
 template <int G>
-__global__ __launch_bounds__(kWeightThreads, 4) void weights_kernel(Params p)
+__global__ __launch_bounds__(kWeightThreads, 3) void weights_kernel(Params p)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-    Plan plan = make_plan<false>(p, kWeightPairCost, blockIdx.x, lane);
+    // neighbouring heads of the same blocks on the waves of a work group
+    __shared__ __attribute__((aligned(16))) float s_sums[kWeightWaves][kChunk * kBlockSize];
+    const int together = p.Hkv % 4 == 0 ? 4 : p.Hkv % 2 == 0 ? 2 : 1;
+    const int groups = p.Hkv / together;
+    Plan plan = make_plan<false>(p, groups, kWeightPairCost, blockIdx.x, lane);
     bool more = plan.take > 0;
     while (more) {
-        const Span s = wave_span(p, plan.b, plan.g, plan.L, plan.blk, plan.blk + plan.take, wave, kWeightThreads / 64);
-        if (s.n > 0) accumulate<G>(p, plan.b, plan.g, s, lane);
-        more = next_segment(p, kWeightPairCost, plan);
+        const int g = plan.g * together + wave % together;
+        const Span s = wave_span(p, plan.b, g, plan.L, plan.blk, plan.blk + plan.take, wave / together, kWeightWaves / together);
+        if (s.n > 0) accumulate<G>(p, plan.b, g, s, lane, s_sums[wave]);
+        more = next_segment(p, groups, kWeightPairCost, plan);
     }
 }
 
