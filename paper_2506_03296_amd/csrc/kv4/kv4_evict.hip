@@ -1,27 +1,31 @@
 // kv4_evict.hip -- eviction from the 4-bit KV cache (include/apex_kv4.h).
 //
-// A token's key is 32 bits whose order is the order of keeping: all ones for a
-// protected token, else its weight's bits made monotonic.  select_kernel finds,
-// for one (request, kv-head) pair per work group, the key of the last token
-// kept, digit by digit from the top (counts of a digit's values among the keys
-// that agree so far), and writes a mask, one bit per slot.  move_kernel reads
-// the masks only, so it may overwrite weights and positions: the i-th evicted
-// slot below `keep` takes the i-th kept one from `keep` on.  Sources and targets
-// are disjoint, so the moves need no order, and a cut by a few tokens moves a
-// few rows.
+// The order of keeping is the order of 64-bit numbers: a token's key (all ones
+// for a protected token, else its weight's bits made monotonic) above its slot
+// inverted, so no two are equal.  One work group per (request, kv-head) pair
+// finds the keep-th of them: counts of the top digit's values among the
+// candidates, the digit that holds it, the next digit among those, until few
+// candidates are left, which are ranked against each other.  A thread keeps its
+// keys in registers up to kResident tokens a pair, so weights and positions are
+// read once; longer pairs read them again for every digit.
+//
+// What is kept goes into a mask, one bit per slot, and the moves are read off
+// the masks only (they overwrite weights and positions): the i-th evicted slot
+// below `keep` takes the i-th kept one from `keep` on.  Sources and targets are
+// disjoint, so the moves need no order, and a cut by a few tokens moves a few
+// rows.
 #include "kv4_host.h"
 
 namespace {
 
 using namespace kv4;
 
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int kSelectThreads = 1024;
-constexpr int kSelectWaves = kSelectThreads / 64;
 constexpr int kBins = 2048;
-constexpr int kMoveThreads = 256;
-constexpr int kMoves = 256;        // moves of a work group at a time
+constexpr int kFew = 256;                  // candidates that are ranked directly
+constexpr int kMostPerThread = 32;         // keys that a thread keeps
+constexpr int kAgainPerThread = 16;        // and reads at a time where it keeps none
+constexpr int kSmall = 256, kLarge = 1024; // threads of a work group
+constexpr int kOwnMoves = 1024;
 
 struct EvictParams {
     char* cache;
@@ -30,10 +34,11 @@ struct EvictParams {
     float* weights;
     int32_t* positions;
     uint64_t* masks;       // [B][Hkv][words], bit i of word w: slot 64 w + i is kept
-    int32_t* counts;       // [B][Hkv] tokens to move
-    int64_t num_blocks;
+    int32_t* counts;       // [B][Hkv] tokens left to move
+    unsigned num_blocks;
     int Hkv, stride, words;
     int keep, sinks, recent;
+    int own_moves;         // select_kernel moves up to so many tokens of a pair itself
 };
 
 __device__ inline int context(const EvictParams& p, int b)
@@ -43,12 +48,10 @@ __device__ inline int context(const EvictParams& p, int b)
     return L > row ? (int)row : L;
 }
 
-// Index of slot t of pair (b, g) in weights and positions; -1 for a block
-// outside the pool.
-__device__ inline int64_t slot_index(const EvictParams& p, const int32_t* row, int g, int t)
+// Index of a slot in weights and positions from its block id; -1 outside the pool.
+__device__ inline int64_t slot_index(const EvictParams& p, int id, int g, int t)
 {
-    const int id = row[t / kBlockSize];
-    return id >= 0 && (int64_t)id < p.num_blocks ? ((int64_t)id * p.Hkv + g) * kBlockSize + t % kBlockSize : -1;
+    return (unsigned)id < p.num_blocks ? ((int64_t)id * p.Hkv + g) * kBlockSize + t % kBlockSize : -1;
 }
 
 // Order-preserving bits of a weight; below every protected token's.
@@ -57,13 +60,6 @@ __device__ inline unsigned weight_key(float w)
     if (w != w) w = -INFINITY;
     const unsigned u = __float_as_uint(w + 0.f);   // (-0 becomes 0)
     return (u >> 31) ? ~u : u | 0x80000000u;
-}
-
-__device__ inline int wave_sum(int x)
-{
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m, 64);
-    return x;
 }
 
 // Inclusive sum over the lanes of a wave.
@@ -77,178 +73,367 @@ __device__ inline int wave_scan(int x, int lane)
     return x;
 }
 
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictParams p)
-{
-    __shared__ unsigned s_bins[kBins];
-    __shared__ int s_wave[kSelectWaves];
-    __shared__ unsigned s_digit;
-    __shared__ int s_above;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int b = (int)blockIdx.x / p.Hkv, g = (int)blockIdx.x - b * p.Hkv;
-    const int L = context(p, b);
-    if (L <= p.keep) {
-        if (tid == 0) p.counts[blockIdx.x] = 0;
-        return;
-    }
-    const int32_t* row = p.bt + (int64_t)b * p.stride;
+// --- moves ------------------------------------------------------------------------
 
-    // the newest position
+template <int kN>
+struct Moves {
+    int64_t to[kN], from[kN];   // slot indexes
+    int holes[kN / 64], movers[kN / 64];
+};
+
+// Moves r0 .. r0 + kN of a pair's n, by kN threads.
+template <int kN>
+__device__ inline void move_rows(const EvictParams& p, const int32_t* row, int g, const uint64_t* kept, int L, int r0, int n,
+                                 Moves<kN>& sh)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, keep = p.keep;
+    // a thread counts the holes (evicted below keep) and movers (kept from keep
+    // on) of consecutive words, a scan ranks them, then it lists its own
+    const int words = (L + 63) / 64, per = (words + kN - 1) / kN;
+    const int a = min(words, tid * per), e = min(words, a + per);
+    auto below = [&](int w) -> uint64_t {   // bits of the word's slots below keep
+        const int left = keep - w * 64;
+        return left <= 0 ? 0ull : left >= 64 ? ~0ull : (1ull << left) - 1;
+    };
+    int holes = 0, movers = 0;
+    for (int w = a; w < e; ++w) {
+        const uint64_t k = kept[w], low = below(w);
+        holes += __popcll(~k & low);
+        movers += __popcll(k & ~low);
+    }
+    int hole = wave_scan(holes, lane), mover = wave_scan(movers, lane);
+    if (lane == 63) {
+        sh.holes[wave] = hole;
+        sh.movers[wave] = mover;
+    }
+    sh.to[tid] = sh.from[tid] = -1;
+    __syncthreads();
+    for (int i = 0; i < wave; ++i) {
+        hole += sh.holes[i];
+        mover += sh.movers[i];
+    }
+    hole -= holes + r0;
+    mover -= movers + r0;
+    for (int w = a; w < e; ++w) {
+        const uint64_t k = kept[w], low = below(w);
+        uint64_t m = ~k & low;
+        if (hole + __popcll(m) <= 0 || hole >= kN)
+            hole += __popcll(m);
+        else
+            for (; m; m &= m - 1, ++hole)
+                if (hole >= 0 && hole < kN) sh.to[hole] = w * 64 + __builtin_ctzll(m);
+        m = k & ~low;
+        if (mover + __popcll(m) <= 0 || mover >= kN)
+            mover += __popcll(m);
+        else
+            for (; m; m &= m - 1, ++mover)
+                if (mover >= 0 && mover < kN) sh.from[mover] = w * 64 + __builtin_ctzll(m);
+    }
+    __syncthreads();
+    // slots to indexes, one pair a thread
+    const int64_t to_slot = sh.to[tid], from_slot = sh.from[tid];
+    if (to_slot >= 0 && from_slot >= 0) {
+        const int to_id = row[to_slot / kBlockSize], from_id = row[from_slot / kBlockSize];
+        sh.to[tid] = slot_index(p, to_id, g, (int)to_slot);
+        sh.from[tid] = slot_index(p, from_id, g, (int)from_slot);
+    }
+    __syncthreads();
+    // 16 lanes a move, kAtOnce moves a thread on their way: lane c has 4 bytes of
+    // K and dims [8c, 8c + 8) of V; lanes 0-3 V's scales, 4 K's, 5 and 6 weight
+    // and position
+    constexpr int kAtOnce = 4, kLanes = 16, kStep = kN / kLanes;
+    const int c = tid % kLanes, m1 = min(kN, n - r0);
+    for (int m0 = tid / kLanes; m0 < m1; m0 += kStep * kAtOnce) {
+        unsigned k[kAtOnce], v[kAtOnce], x[kAtOnce];
+        int64_t to[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int m = m0 + i * kStep;
+            const int64_t from = m < m1 ? sh.from[m] : -1;
+            to[i] = m < m1 && from >= 0 ? sh.to[m] : -1;
+            if (to[i] < 0) continue;
+            const int fi = (int)(from % kBlockSize);
+            const char* fs = p.cache + from / kBlockSize * kSlabBytes;
+            k[i] = *(const unsigned*)(fs + fi * 64 + c * 4);
+            v[i] = *(const unsigned*)(fs + v_code_offset(fi, c));
+            if (c < 4)
+                x[i] = *(const unsigned char*)(fs + kVScales + c * kBlockSize + fi);
+            else if (c < 7)
+                x[i] = *(c == 4 ? (const unsigned*)(fs + kKScales + fi * 4)
+                                : c == 5 ? (const unsigned*)p.weights + from : (const unsigned*)p.positions + from);
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (to[i] < 0) continue;
+            const int ti = (int)(to[i] % kBlockSize);
+            char* ts = p.cache + to[i] / kBlockSize * kSlabBytes;
+            *(unsigned*)(ts + ti * 64 + c * 4) = k[i];
+            *(unsigned*)(ts + v_code_offset(ti, c)) = v[i];
+            if (c < 4)
+                *(unsigned char*)(ts + kVScales + c * kBlockSize + ti) = (unsigned char)x[i];
+            else if (c < 7)
+                *(c == 4 ? (unsigned*)(ts + kKScales + ti * 4)
+                         : c == 5 ? (unsigned*)p.weights + to[i] : (unsigned*)p.positions + to[i]) = x[i];
+        }
+    }
+}
+
+__global__ __launch_bounds__(kSmall) void move_kernel(EvictParams p)
+{
+    __shared__ Moves<kSmall> sh;
+    const int pair = (int)blockIdx.x, b = pair / p.Hkv, g = pair - b * p.Hkv;
+    const int n = p.counts[pair], L = context(p, b);
+    for (int r0 = (int)blockIdx.y * kSmall; r0 < n; r0 += (int)gridDim.y * kSmall) {
+        move_rows<kSmall>(p, p.bt + (int64_t)b * p.stride, g, p.masks + (int64_t)pair * p.words, L, r0, n, sh);
+        __syncthreads();
+    }
+}
+
+// --- selection --------------------------------------------------------------------
+
+struct Select {
+    unsigned bins[kBins];
+    uint64_t few[kFew];
+    int wave[kLarge / 64];
+    unsigned digit;
+    int above, count, few_n;
+    uint64_t last;
+};
+
+// Keys of tokens first + kT i + tid, i < kN, in two steps: what is read, and
+// (once the newest position is known) the keys.  A slot past L or of a block
+// outside the pool reads slot 0's values and has key 0.
+template <int kT, int kN>
+struct Tokens {
+    unsigned w[kN];     // weights' bits, then keys
+    int pos[kN];
+    unsigned live;      // bit i
+    __device__ inline void load(const EvictParams& p, const int32_t* row, int g, int L, int first)
+    {
+        static_assert(kN <= 32, "a bit for every token");
+        const int tid = (int)threadIdx.x;
+        int id[kN];
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const int t = first + i * kT + tid;
+            id[i] = row[t < L ? t / kBlockSize : 0];
+        }
+        live = 0;
+        const int64_t at0 = (int64_t)g * kBlockSize + tid % kBlockSize;   // (kT is a multiple of the block)
+        const int64_t step = (int64_t)p.Hkv * kBlockSize;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const bool ok = first + i * kT + tid < L && (unsigned)id[i] < p.num_blocks;
+            live |= ok ? 1u << i : 0u;
+            const int64_t at = at0 + (ok ? id[i] : 0) * step;
+            pos[i] = p.positions[at];
+            w[i] = __float_as_uint(p.weights[at]);
+        }
+    }
+    __device__ inline int newest() const
+    {
+        int n = INT_MIN;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) n = max(n, live >> i & 1 ? pos[i] : INT_MIN);
+        return n;
+    }
+    __device__ inline void keys(int sinks, int64_t recent_from)
+    {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const bool safe = pos[i] < sinks || (int64_t)pos[i] > recent_from;
+            w[i] = !(live >> i & 1) ? 0u : safe ? 0xffffffffu : weight_key(__uint_as_float(w[i]));
+        }
+    }
+};
+
+template <int kT, int kN, bool kAgain>
+__device__ inline void select_pair(const EvictParams& p, const int32_t* row, int g, int L, uint64_t* out, Select& sh)
+{
+    constexpr int kWaves = kT / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    Tokens<kT, kN> x;
     int newest = INT_MIN;
-    for (int t = tid; t < L; t += kSelectThreads) {
-        const int64_t i = slot_index(p, row, g, t);
-        if (i >= 0) newest = max(newest, p.positions[i]);
+    for (int first = 0; first == 0 || (kAgain && first < L); first += kN * kT) {
+        x.load(p, row, g, L, first);
+        newest = max(newest, x.newest());
     }
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) newest = max(newest, __shfl_xor(newest, m, 64));
-    if (lane == 0) s_wave[wave] = newest;
+    if (lane == 0) sh.wave[wave] = newest;
     __syncthreads();
-    for (int i = 0; i < kSelectWaves; ++i) newest = max(newest, s_wave[i]);
+    for (int i = 0; i < kWaves; ++i) newest = max(newest, sh.wave[i]);
     const int64_t recent_from = (int64_t)newest - p.recent;
-
-    auto key_of = [&](int t) -> unsigned {
-        const int64_t i = slot_index(p, row, g, t);
-        if (i < 0) return 0u;
-        const int pos = p.positions[i];
-        return pos < p.sinks || (int64_t)pos > recent_from ? 0xffffffffu : weight_key(p.weights[i]);
+    if (!kAgain) x.keys(p.sinks, recent_from);
+    // f(key, t, i) for every token, the i-th of its thread's batch, then g(first)
+    // for the batch.  Slots past L take part: they have key 0 and come after every
+    // token, so the keep-th is none of them.
+    auto walk = [&](auto f, auto batch) {
+        for (int first = 0; first == 0 || (kAgain && first < L); first += kN * kT) {
+            if (kAgain) {
+                x.load(p, row, g, L, first);
+                x.keys(p.sinks, recent_from);
+            }
+#pragma unroll
+            for (int i = 0; i < kN; ++i) f(x.w[i], first + i * kT + tid, i);
+            batch(first);
+        }
+    };
+    auto no_batch = [](int) {};
+    // counts of a digit of the tokens that are `in`, then the digit that holds the
+    // need-th from the top
+    const int all = (L + kN * kT - 1) / (kN * kT) * (kN * kT);
+    int need = p.keep, candidates = all;
+    auto find_digit = [&](auto in, auto digit) -> unsigned {
+        for (int i = tid; i < kBins; i += kT) sh.bins[i] = 0;
+        __syncthreads();
+        if (candidates < all && candidates > all / 2) {
+            // most tokens share the digits so far, so mostly the next one too
+            // (equal weights): a wave whose candidates have one digit counts once
+            walk([&](unsigned key, int t, int) {
+                const bool c = in(key, t);
+                const unsigned d = digit(key, t);
+                const uint64_t act = __ballot(c);
+                const unsigned d0 = (unsigned)__builtin_amdgcn_readlane((int)d, act ? __builtin_ctzll(act) : 0);
+                if (__ballot(c && d != d0) == 0) {
+                    if (lane == 0 && act) atomicAdd(&sh.bins[d0], (unsigned)__popcll(act));
+                } else if (c) {
+                    atomicAdd(&sh.bins[d], 1u);
+                }
+            }, no_batch);
+        } else {
+            walk([&](unsigned key, int t, int) {
+                if (in(key, t)) atomicAdd(&sh.bins[digit(key, t)], 1u);
+            }, no_batch);
+        }
+        __syncthreads();
+        // a thread has kPer bins, counted down from the top: the counts above them
+        constexpr int kPer = kBins / kT;
+        const int top = kBins - 1 - kPer * tid;
+        int c[kPer], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) sum += c[i] = (int)sh.bins[top - i];
+        int incl = wave_scan(sum, lane);
+        if (lane == 63) sh.wave[wave] = incl;
+        __syncthreads();
+        for (int i = 0; i < wave; ++i) incl += sh.wave[i];
+        int above = incl - sum;
+        if (above < need && need <= incl) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                if (above < need && need <= above + c[i]) {
+                    sh.digit = (unsigned)(top - i);
+                    sh.above = above;
+                    sh.count = c[i];
+                }
+                above += c[i];
+            }
+        }
+        __syncthreads();
+        need -= sh.above;
+        candidates = sh.count;
+        return sh.digit;
     };
 
-    // the key of the keep-th token in the order of keeping: 11, 11 and 10 bits
-    unsigned prefix = 0, mask = 0;
-    int need = p.keep;   // tokens to keep among those that agree with prefix
-    for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        for (int i = tid; i < kBins; i += kSelectThreads) s_bins[i] = 0;
-        __syncthreads();
-        for (int t = tid; t < L; t += kSelectThreads) {
-            const unsigned k = key_of(t);
-            if ((k & mask) == prefix) atomicAdd(&s_bins[(k >> shift) & ((1u << bits) - 1)], 1u);
-        }
-        __syncthreads();
-        // thread i has bins 2 i' and 2 i' + 1, from the top: counts above a bin
-        const int top = kBins - 1 - 2 * tid;
-        const int c0 = (int)s_bins[top], c1 = (int)s_bins[top - 1];
-        int incl = wave_scan(c0 + c1, lane);
-        if (lane == 63) s_wave[wave] = incl;
-        __syncthreads();
-        for (int i = 0; i < wave; ++i) incl += s_wave[i];
-        const int above = incl - c0 - c1;
-        if (above < need && need <= above + c0) {
-            s_digit = (unsigned)top;
-            s_above = above;
-        } else if (above + c0 < need && need <= incl) {
-            s_digit = (unsigned)top - 1;
-            s_above = above + c0;
-        }
-        __syncthreads();
-        prefix |= s_digit << shift;
-        mask |= ((1u << bits) - 1) << shift;
-        need -= s_above;
+    // the keep-th key from the top, digit by digit: candidates have key >> shift
+    // == prefix.  Should more than kFew have the whole key, the same for their
+    // slots, inverted: last_slot >> slot_shift of the candidates
+    unsigned prefix = 0, slots = 0;
+    int shift = 32, slot_shift = 32;   // (32: no digit yet)
+    auto in_keys = [&](unsigned key, int) -> bool { return key >> shift == prefix; };
+    auto in_slots = [&](unsigned key, int t) -> bool {
+        return key == prefix && (slot_shift == 32 || ~(unsigned)t >> slot_shift == slots);
+    };
+    if (candidates > kFew) {
+        prefix = find_digit([](unsigned, int) -> bool { return true; }, [](unsigned key, int) -> unsigned { return key >> 21; });
+        shift = 21;
     }
-    // kept: keys above prefix, and the first `need` (in slot order) that equal it
-    uint64_t* out = p.masks + (int64_t)blockIdx.x * p.words;
-    int equal_before = 0, moved = 0;
-    for (int t0 = 0; t0 < L; t0 += kSelectThreads) {
-        const int t = t0 + tid;
-        const unsigned k = t < L ? key_of(t) : 0u;
-        const bool eq = t < L && k == prefix;
-        const uint64_t eqs = __ballot(eq);
-        __syncthreads();
-        if (lane == 0) s_wave[wave] = __popcll(eqs);
-        __syncthreads();
-        int before = equal_before;
-        for (int i = 0; i < kSelectWaves; ++i) {
-            before += i < wave ? s_wave[i] : 0;
-            equal_before += s_wave[i];
-        }
-        const int rank = before + __popcll(eqs & ((1ull << lane) - 1));
-        const bool kept = t < L && (k > prefix || (eq && rank < need));
-        const uint64_t bits = __ballot(kept);
-        moved += kept && t >= p.keep;
-        if (lane == 0 && t < L) out[t >> 6] = bits;
+    while (candidates > kFew && shift > 0) {
+        const int to = shift == 21 ? 10 : 0;
+        const unsigned dm = to == 0 ? 1023u : 2047u;
+        const unsigned d = find_digit(in_keys, [&](unsigned key, int) -> unsigned { return key >> to & dm; });
+        prefix = prefix << (shift - to) | d;
+        shift = to;
     }
-    moved = wave_sum(moved);
+    while (candidates > kFew) {   // (slots differ: it ends)
+        const int to = slot_shift == 32 ? 21 : slot_shift == 21 ? 10 : 0;
+        const unsigned dm = to == 0 ? 1023u : 2047u;
+        const unsigned d = find_digit(in_slots, [&](unsigned, int t) -> unsigned { return ~(unsigned)t >> to & dm; });
+        slots = slot_shift == 32 ? d : slots << (slot_shift - to) | d;
+        slot_shift = to;
+    }
+    // rank the candidates by key, then slot
+    if (tid == 0) sh.few_n = 0;
     __syncthreads();
-    if (lane == 0) s_wave[wave] = moved;
+    walk([&](unsigned key, int t, int) {
+        const bool c = shift == 32 || (slot_shift < 32 ? in_slots(key, t) : in_keys(key, t));
+        if (c) sh.few[atomicAdd(&sh.few_n, 1)] = (uint64_t)key << 32 | ~(unsigned)t;
+    }, no_batch);
     __syncthreads();
-    if (tid == 0) {
-        int n = 0;
-        for (int i = 0; i < kSelectWaves; ++i) n += s_wave[i];
-        p.counts[blockIdx.x] = n;
+    for (int i = tid; i < candidates; i += kT) {
+        const uint64_t o = sh.few[i];
+        int r = 0;
+        for (int j = 0; j < candidates; ++j) r += sh.few[j] > o;
+        if (r == need - 1) sh.last = o;
     }
+    __syncthreads();
+    const unsigned last_key = (unsigned)(sh.last >> 32);
+    const int last_t = (int)~(unsigned)sh.last;
+    // lane i of a wave gets the mask of the wave's i-th 64 slots
+    int moved = 0;
+    unsigned lo = 0, hi = 0;
+    walk([&](unsigned key, int t, int i) {
+        const uint64_t bits = __ballot(key > last_key || (key == last_key && t <= last_t));
+        lo = lane == i ? (unsigned)bits : lo;
+        hi = lane == i ? (unsigned)(bits >> 32) : hi;
+    }, [&](int first) {
+        const int t = first + lane * kT + wave * 64;
+        if (lane < kN && t < L) {
+            const uint64_t bits = (uint64_t)hi << 32 | lo;
+            out[t >> 6] = bits;
+            const int skip = p.keep - t;
+            moved += __popcll(bits & (skip <= 0 ? ~0ull : skip >= 64 ? 0ull : ~0ull << skip));
+        }
+    });
+    moved = wave_scan(moved, lane);
+    if (lane == 63) sh.wave[wave] = moved;
+    __syncthreads();
 }
 
-// The slots with ranks [r0, r0 + kMoves) among the set bits of f(word), words
-// [w0, w1), into list; every thread of the work group takes part.
-template <typename F>
-__device__ inline void list_slots(int w0, int w1, int r0, int* list, int* s_wave, F f)
+template <int kT>
+__global__ __launch_bounds__(kT, 4) void select_kernel(EvictParams p)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int per = (w1 - w0 + kMoveThreads - 1) / kMoveThreads;
-    const int a = min(w1, w0 + tid * per), e = min(w1, a + per);
-    int n = 0;
-    for (int w = a; w < e; ++w) n += __popcll(f(w));
-    int rank = wave_scan(n, lane);
-    __syncthreads();
-    if (lane == 63) s_wave[wave] = rank;
-    __syncthreads();
-    for (int i = 0; i < wave; ++i) rank += s_wave[i];
-    rank -= n;
-    for (int w = a; w < e && rank < r0 + kMoves; ++w) {
-        uint64_t m = f(w);
-        const int c = __popcll(m);
-        if (rank + c <= r0) {
-            rank += c;
-            continue;
-        }
-        for (; m; m &= m - 1, ++rank)
-            if (rank >= r0 && rank < r0 + kMoves) list[rank - r0] = w * 64 + __builtin_ctzll(m);
-    }
-}
-
-__global__ __launch_bounds__(kMoveThreads) void move_kernel(EvictParams p)
-{
-    __shared__ int s_to[kMoves], s_from[kMoves];
-    __shared__ int s_wave[kMoveThreads / 64];
-    const int tid = threadIdx.x;
+    __shared__ union {
+        Select select;
+        Moves<kT> moves;
+    } sh;
     const int pair = (int)blockIdx.x, b = pair / p.Hkv, g = pair - b * p.Hkv;
-    const int n = p.counts[pair];
     const int L = context(p, b);
-    const uint64_t* kept = p.masks + (int64_t)pair * p.words;
+    if (L <= p.keep) {
+        if (threadIdx.x == 0) p.counts[pair] = 0;
+        return;
+    }
     const int32_t* row = p.bt + (int64_t)b * p.stride;
-    for (int r0 = (int)blockIdx.y * kMoves; r0 < n; r0 += (int)gridDim.y * kMoves) {
-        const int keep = p.keep;
-        list_slots(0, (keep + 63) / 64, r0, s_to, s_wave, [&](int w) -> uint64_t {
-            const int left = keep - w * 64;
-            return ~kept[w] & (left >= 64 ? ~0ull : (1ull << left) - 1);
-        });
-        list_slots(keep / 64, (L + 63) / 64, r0, s_from, s_wave, [&](int w) -> uint64_t {
-            const int skip = keep - w * 64;
-            return kept[w] & (skip <= 0 ? ~0ull : ~0ull << skip);
-        });
+    uint64_t* out = p.masks + (int64_t)pair * p.words;
+    if (L <= 2 * kT)
+        select_pair<kT, 2, false>(p, row, g, L, out, sh.select);
+    else if (L <= 8 * kT)
+        select_pair<kT, 8, false>(p, row, g, L, out, sh.select);
+    else if (L <= 16 * kT)
+        select_pair<kT, 16, false>(p, row, g, L, out, sh.select);
+    else if (L <= kMostPerThread * kT)
+        select_pair<kT, kMostPerThread, false>(p, row, g, L, out, sh.select);
+    else
+        select_pair<kT, kAgainPerThread, true>(p, row, g, L, out, sh.select);
+    int n = 0;
+    for (int i = 0; i < kT / 64; ++i) n += sh.select.wave[i];
+    const bool own = n <= p.own_moves;
+    if (threadIdx.x == 0) p.counts[pair] = own ? 0 : n;
+    if (!own) return;
+    // (the masks are this work group's own: the barrier makes them visible)
+    for (int r0 = 0; r0 < n; r0 += kT) {
         __syncthreads();
-        // 16 lanes a move: lane c has 4 bytes of K, dims [8c, 8c + 8) of V
-        const int c = tid & 15, m1 = min(kMoves, n - r0);
-        for (int m = tid >> 4; m < m1; m += kMoveThreads / 16) {
-            const int64_t to = slot_index(p, row, g, s_to[m]), from = slot_index(p, row, g, s_from[m]);
-            if (to < 0 || from < 0) continue;
-            const int ti = (int)(to % kBlockSize), fi = (int)(from % kBlockSize);
-            char* ts = p.cache + to / kBlockSize * kSlabBytes;
-            const char* fs = p.cache + from / kBlockSize * kSlabBytes;
-            const unsigned k = *(const unsigned*)(fs + fi * 64 + c * 4), v = *(const unsigned*)(fs + v_code_offset(fi, c));
-            if (c < 4) {
-                const char s = fs[kVScales + c * kBlockSize + fi];
-                ts[kVScales + c * kBlockSize + ti] = s;
-            } else if (c == 4) {
-                *(unsigned*)(ts + kKScales + ti * 4) = *(const unsigned*)(fs + kKScales + fi * 4);
-            } else if (c == 5) {
-                p.weights[to] = p.weights[from];
-            } else if (c == 6) {
-                p.positions[to] = p.positions[from];
-            }
-            *(unsigned*)(ts + ti * 64 + c * 4) = k;
-            *(unsigned*)(ts + v_code_offset(ti, c)) = v;
-        }
-        __syncthreads();
+        move_rows<kT>(p, row, g, out, L, r0, n, sh.moves);
     }
 }
 
@@ -302,7 +487,11 @@ extern "C" int apex_kv4_evict(void* kv_cache, const int32_t* block_table, int64_
     rc = workspace ? check_workspace(workspace, workspace_bytes, need)
                    : library_buffer(kMasks, need, (hipStream_t)stream, &workspace);
     if (rc != APEX_OK) return rc;
-    if (block_table_stride * kBlockSize <= keep) return APEX_OK;   // no request can be longer
+    const int64_t longest = block_table_stride * kBlockSize;
+    if (longest <= keep || num_blocks == 0) return APEX_OK;   // no request can be longer, no token is in the pool
+    int cus = 0;
+    rc = compute_units(&cus);
+    if (rc != APEX_OK) return rc;
     EvictParams p;
     p.cache = (char*)kv_cache;
     p.bt = block_table;
@@ -311,20 +500,26 @@ extern "C" int apex_kv4_evict(void* kv_cache, const int32_t* block_table, int64_
     p.positions = positions;
     p.counts = (int32_t*)workspace;
     p.masks = (uint64_t*)((char*)workspace + count_bytes(B, Hkv));
-    p.num_blocks = num_blocks;
+    p.num_blocks = (unsigned)num_blocks;
     p.Hkv = Hkv;
     p.stride = (int)block_table_stride;
     p.words = (int)mask_words(block_table_stride);
     p.keep = keep;
     p.sinks = sinks;
     p.recent = recent;
-    const unsigned pairs = (unsigned)(B * Hkv);
-    select_kernel<<<pairs, kSelectThreads, 0, (hipStream_t)stream>>>(p);
-    if ((rc = launched("kv4 evict")) != APEX_OK) return rc;
-    // at most min(keep, longest - keep) tokens of a pair move
-    const int64_t longest = block_table_stride * kBlockSize, most = longest - keep < keep ? longest - keep : keep;
-    int64_t groups = (most + kMoves - 1) / kMoves;
+    const int pairs = B * Hkv;
+    // at most min(keep, longest - keep) tokens of a pair move.  Up to kOwnMoves
+    // are moved by the work group that selects them; a second launch spreads what
+    // is left.
+    const int64_t most = longest - keep < keep ? longest - keep : keep;
+    p.own_moves = kOwnMoves;
+    if (longest <= kMostPerThread * kSmall || pairs >= 4 * cus)
+        select_kernel<kSmall><<<(unsigned)pairs, kSmall, 0, (hipStream_t)stream>>>(p);
+    else
+        select_kernel<kLarge><<<(unsigned)pairs, kLarge, 0, (hipStream_t)stream>>>(p);
+    if ((rc = launched("kv4 evict")) != APEX_OK || most <= kOwnMoves) return rc;
+    int64_t groups = (most + kSmall - 1) / kSmall;
     if (groups * pairs > 4096) groups = 4096 / pairs > 0 ? 4096 / pairs : 1;
-    move_kernel<<<dim3(pairs, (unsigned)groups), kMoveThreads, 0, (hipStream_t)stream>>>(p);
+    move_kernel<<<dim3((unsigned)pairs, (unsigned)groups), kSmall, 0, (hipStream_t)stream>>>(p);
     return launched("kv4 evict");
 }
