@@ -5,7 +5,9 @@
 // quad permutes away.  A wave takes four consecutive tokens of one kv-head and
 // a work group sixteen: where they lie in consecutive slots, as a prompt's do,
 // a wave's codes are 256 contiguous bytes of K and of V, and the work group
-// writes (or reads) a whole slab.
+// writes (or reads) whole slabs.  Bound by HBM for prompts (5.4 TB/s of reads
+// and writes together; a large copy has 4.8), by the launch and two round trips
+// for a decode step.
 #include "kv4_host.h"
 
 namespace {
@@ -17,7 +19,14 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256;
 constexpr int kRowLanes = 16;
-constexpr int kTokens = kThreads / kRowLanes;   // tokens of a work group
+// fp16 rows up to half the 256 MB Infinity Cache are read and written through
+// it: they come out of a projection that has just written them, or go to a
+// reader that comes next.  More would not stay there and goes past it (54 000
+// tokens of 8 kv-heads, 224 MB: appended in 51 us, 58 through it, read back in
+// 40, 49 through it).
+constexpr size_t kCachedBytes = (size_t)128 << 20;
+constexpr int kTokens = kThreads / kRowLanes;   // tokens of a work group at a time
+constexpr int kRows = 2;                        // and how many times
 
 __device__ inline f16x2 as_h2(unsigned u) { return __builtin_bit_cast(f16x2, u); }
 
@@ -78,71 +87,110 @@ struct RowShape {
     int64_t token_stride;   // bytes between tokens of the new rows
 };
 
-// Group (16 tokens, kv-head) of a work group; heads fastest, so that the work
-// groups of the same tokens run together.
-__device__ inline bool row_of(const RowShape& s, int64_t& t, int& g, int& c)
+// A work group's tokens and head: heads fastest, so that the work groups of the
+// same tokens run together.  A lane takes piece c of rows t, t + kTokens, ...
+struct RowPlace {
+    int64_t t;
+    int g, c;
+};
+
+__device__ inline RowPlace row_place(const RowShape& s)
 {
-    const unsigned group = blockIdx.x;
-    const unsigned chunk = group / (unsigned)s.Hkv;
-    g = (int)(group - chunk * (unsigned)s.Hkv);
-    t = (int64_t)chunk * kTokens + threadIdx.x / kRowLanes;
-    c = threadIdx.x % kRowLanes;
-    return t < s.T;
+    const unsigned group = blockIdx.x, chunk = group / (unsigned)s.Hkv;
+    return {(int64_t)chunk * (kTokens * kRows) + threadIdx.x / kRowLanes, (int)(group - chunk * (unsigned)s.Hkv),
+            (int)(threadIdx.x % kRowLanes)};
 }
 
+// Slots of a lane's rows, -1 outside the pool: all are asked for before the
+// first is needed, and rows only once their slot is known (padding costs its
+// slot and nothing else).
+__device__ inline void load_slots(const int64_t* slots, const RowShape& s, int64_t t, int64_t (&slot)[kRows])
+{
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t at = t + i * kTokens;
+        slot[i] = at < s.T ? slots[at] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+        if (slot[i] >= s.capacity) slot[i] = -1;
+}
+
+template <bool kStream>
 __global__ __launch_bounds__(kThreads) void append_kernel(const char* __restrict__ k_new, const char* __restrict__ v_new,
                                                           char* __restrict__ cache, const int64_t* __restrict__ slots,
                                                           const int32_t* __restrict__ token_positions,
                                                           int32_t* __restrict__ positions, float* __restrict__ weights,
                                                           RowShape s)
 {
-    int64_t t;
-    int g, c;
-    if (!row_of(s, t, g, c)) return;
-    const int64_t slot = slots[t];
-    if (slot < 0 || slot >= s.capacity) return;   // (all 16 lanes of a row)
-    const int64_t from = t * s.token_stride + (int64_t)g * (kHeadDim * 2) + c * 16;
-    const u32x4 k = *(const u32x4*)(k_new + from), v = *(const u32x4*)(v_new + from);
-    int ks, vs;
-    const unsigned kc = quantise(k, ks), vc = quantise(v, vs);
-    const int64_t row = (slot / kBlockSize) * s.Hkv + g;
-    const int at = (int)(slot % kBlockSize);
-    char* slab = cache + row * kSlabBytes;
-    *(unsigned*)(slab + at * 64 + c * 4) = kc;
-    *(unsigned*)(slab + v_code_offset(at, c)) = vc;
-    if ((c & 3) == 0) {
-        slab[kKScales + at * 4 + (c >> 2)] = (char)ks;
-        slab[kVScales + (c >> 2) * kBlockSize + at] = (char)vs;
+    const RowPlace r = row_place(s);
+    int64_t slot[kRows];
+    load_slots(slots, s, r.t, slot);
+    u32x4 k[kRows], v[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        if (slot[i] < 0) continue;   // (all 16 lanes of a row)
+        const int64_t from = (r.t + i * kTokens) * s.token_stride + (int64_t)r.g * (kHeadDim * 2) + r.c * 16;
+        k[i] = kStream ? __builtin_nontemporal_load((const u32x4*)(k_new + from)) : *(const u32x4*)(k_new + from);
+        v[i] = kStream ? __builtin_nontemporal_load((const u32x4*)(v_new + from)) : *(const u32x4*)(v_new + from);
     }
-    if (positions && c == 1) positions[row * kBlockSize + at] = token_positions[t];
-    if (weights && c == 2) weights[row * kBlockSize + at] = 0.f;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        if (slot[i] < 0) continue;
+        int ks, vs;
+        const unsigned kc = quantise(k[i], ks), vc = quantise(v[i], vs);
+        const int64_t row = (slot[i] / kBlockSize) * s.Hkv + r.g;
+        const int at = (int)(slot[i] % kBlockSize), c = r.c;
+        char* slab = cache + row * kSlabBytes;
+        *(unsigned*)(slab + at * 64 + c * 4) = kc;
+        *(unsigned*)(slab + v_code_offset(at, c)) = vc;
+        if ((c & 3) == 0) {
+            slab[kKScales + at * 4 + (c >> 2)] = (char)ks;
+            slab[kVScales + (c >> 2) * kBlockSize + at] = (char)vs;
+        }
+        if (positions && c == 1) positions[row * kBlockSize + at] = token_positions[r.t + i * kTokens];
+        if (weights && c == 2) weights[row * kBlockSize + at] = 0.f;
+    }
 }
 
+template <bool kStream>
 __global__ __launch_bounds__(kThreads) void gather_kernel(const char* __restrict__ cache, const int64_t* __restrict__ slots,
                                                           char* __restrict__ k_out, char* __restrict__ v_out, RowShape s)
 {
-    int64_t t;
-    int g, c;
-    if (!row_of(s, t, g, c)) return;
-    const int64_t slot = slots[t];
-    u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-    if (slot >= 0 && slot < s.capacity) {
-        const char* slab = cache + ((slot / kBlockSize) * s.Hkv + g) * kSlabBytes;
-        const int at = (int)(slot % kBlockSize);
-        const unsigned kc = *(const unsigned*)(slab + at * 64 + c * 4);
-        const unsigned vc = *(const unsigned*)(slab + v_code_offset(at, c));
-        const int ks = *(const unsigned char*)(slab + kKScales + at * 4 + (c >> 2));
-        const int vs = *(const unsigned char*)(slab + kVScales + (c >> 2) * kBlockSize + at);
-        k = dequantise(kc, ks);
-        v = dequantise(vc, vs);
+    const RowPlace r = row_place(s);
+    int64_t slot[kRows];
+    load_slots(slots, s, r.t, slot);
+    unsigned kc[kRows], vc[kRows];
+    int ks[kRows], vs[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        kc[i] = vc[i] = 0;
+        ks[i] = vs[i] = 127;
+        if (slot[i] < 0) continue;
+        const char* slab = cache + ((slot[i] / kBlockSize) * s.Hkv + r.g) * kSlabBytes;
+        const int at = (int)(slot[i] % kBlockSize), c = r.c;
+        kc[i] = *(const unsigned*)(slab + at * 64 + c * 4);
+        vc[i] = *(const unsigned*)(slab + v_code_offset(at, c));
+        ks[i] = *(const unsigned char*)(slab + kKScales + at * 4 + (c >> 2));
+        vs[i] = *(const unsigned char*)(slab + kVScales + (c >> 2) * kBlockSize + at);
     }
-    const int64_t to = (t * s.Hkv + g) * (kHeadDim * 2) + c * 16;
-    *(u32x4*)(k_out + to) = k;
-    *(u32x4*)(v_out + to) = v;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t t = r.t + i * kTokens;
+        if (t >= s.T) continue;
+        const int64_t to = (t * s.Hkv + r.g) * (kHeadDim * 2) + r.c * 16;
+        const u32x4 k = dequantise(kc[i], ks[i]), v = dequantise(vc[i], vs[i]);
+        if (kStream) {
+            __builtin_nontemporal_store(k, (u32x4*)(k_out + to));
+            __builtin_nontemporal_store(v, (u32x4*)(v_out + to));
+        } else {
+            *(u32x4*)(k_out + to) = k;
+            *(u32x4*)(v_out + to) = v;
+        }
+    }
 }
 
-// T rows of Hkv heads in groups of kTokens; a launch holds fewer than 2^32
-// threads.
+// A launch holds fewer than 2^32 threads.
 int check_rows(int T, int Hkv)
 {
     if (T < 0) return fail(APEX_ERR_INVALID_ARG, "T = %d is negative", T);
@@ -151,7 +199,10 @@ int check_rows(int T, int Hkv)
     return APEX_OK;
 }
 
-dim3 row_grid(int T, int Hkv) { return dim3((unsigned)(((int64_t)T + kTokens - 1) / kTokens * Hkv)); }
+dim3 row_grid(int T, int Hkv)
+{
+    return dim3((unsigned)(((int64_t)T + kTokens * kRows - 1) / (kTokens * kRows) * Hkv));
+}
 
 }  // namespace
 
@@ -188,7 +239,8 @@ extern "C" int apex_kv4_append(const void* k_new, const void* v_new, int64_t new
         return rc;
     if (num_blocks == 0) return APEX_OK;   // every slot is out of the pool
     const RowShape s = {T, Hkv, num_blocks * kBlockSize, stride * 2};
-    append_kernel<<<row_grid(T, Hkv), kThreads, 0, (hipStream_t)stream>>>(
+    const auto kernel = 2 * (size_t)T * row * 2 > kCachedBytes ? append_kernel<true> : append_kernel<false>;
+    kernel<<<row_grid(T, Hkv), kThreads, 0, (hipStream_t)stream>>>(
         (const char*)k_new, (const char*)v_new, (char*)kv_cache, slot_mapping, token_positions, positions, weights, s);
     return launched("kv4 append");
 }
@@ -211,7 +263,8 @@ extern "C" int apex_kv4_gather(const void* kv_cache, const int64_t* slot_mapping
                           {"v_out", v_out, out_bytes}};
     if ((rc = check_disjoint(all[2], all, 2)) != APEX_OK || (rc = check_disjoint(all[3], all, 3)) != APEX_OK) return rc;
     const RowShape s = {T, Hkv, num_blocks * kBlockSize, 0};
-    gather_kernel<<<row_grid(T, Hkv), kThreads, 0, (hipStream_t)stream>>>((const char*)kv_cache, slot_mapping,
-                                                                          (char*)k_out, (char*)v_out, s);
+    const auto kernel = 2 * out_bytes > kCachedBytes ? gather_kernel<true> : gather_kernel<false>;
+    kernel<<<row_grid(T, Hkv), kThreads, 0, (hipStream_t)stream>>>((const char*)kv_cache, slot_mapping, (char*)k_out,
+                                                                   (char*)v_out, s);
     return launched("kv4 gather");
 }

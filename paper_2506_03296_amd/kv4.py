@@ -80,12 +80,12 @@ def _check(rc):
 
 def _call(name, index, *args):
     """The entry point, with the tensors' device (its index) current."""
-    f = getattr(load_library(), name)
-    cuda = _torch().cuda
-    if cuda.current_device() == index:
+    f = getattr(_LIB or load_library(), name)
+    torch = _torch()
+    if torch._C._cuda_getDevice() == index:
         rc = f(*args)
     else:
-        with cuda.device(index):
+        with torch.cuda.device(index):
             rc = f(*args)
     if rc:
         _check(rc)
@@ -149,7 +149,7 @@ def _batch(block_table, context_lens, device):
     return B, stride
 
 
-def _queries(q, B, Hkv, device):
+def _queries(q, B, device):
     """Hq."""
     if q.dim() != 3 or q.shape[0] != B or q.shape[2] != HEAD_DIM:
         raise ValueError(f"q must be [B={B}][Hq][{HEAD_DIM}], got {tuple(q.shape)}")
@@ -157,9 +157,38 @@ def _queries(q, B, Hkv, device):
     return q.shape[1]
 
 
+# The checks above cost 2 us of Python where a decode step's calls take 8 in
+# all.  _plain answers the common case -- everything as it must be -- with a few
+# attribute reads; anything else goes through the checks, which raise what they
+# find.
+
+def _plain(q, kv_cache, block_table, context_lens):
+    """(B, Hq, num_blocks, Hkv, entries per table row, device index) if the
+    checks accept the tensors for sure, else None."""
+    torch = _torch()
+    qs, cs, bs = q.shape, kv_cache.shape, block_table.shape
+    if (len(qs) == 3 and len(cs) == 3 and len(bs) == 2 and q.is_cuda and qs[2] == HEAD_DIM and cs[2] == SLAB_BYTES
+            and bs[0] == qs[0] and context_lens.shape == (qs[0],) and q.dtype is torch.float16
+            and kv_cache.dtype is torch.uint8 and block_table.dtype is torch.int32 and context_lens.dtype is torch.int32):
+        i = q.get_device()
+        if (kv_cache.get_device() == i and block_table.get_device() == i and context_lens.get_device() == i
+                and q.is_contiguous() and kv_cache.is_contiguous() and block_table.is_contiguous()
+                and context_lens.is_contiguous()):
+            return qs[0], qs[1], cs[0], cs[1], bs[1], i
+    return None
+
+
+def _step(q, kv_cache, block_table, context_lens):
+    """As _plain, with an error for what is not so."""
+    plain = _plain(q, kv_cache, block_table, context_lens)
+    if plain is not None:
+        return plain
+    nb, Hkv, dev, index = _cache(kv_cache)
+    B, stride = _batch(block_table, context_lens, dev)
+    return B, _queries(q, B, dev), nb, Hkv, stride, index
+
+
 def _workspace(workspace, device):
-    if workspace is None:
-        return None, 0
     if not (_on(workspace, _torch().uint8, device.index) and workspace.is_contiguous()):
         _require(workspace, "workspace", _torch().uint8, device)
     return workspace.data_ptr(), workspace.numel()
@@ -214,7 +243,7 @@ def gather(kv_cache, slot_mapping, k_out=None, v_out=None, stream=None):
     else:
         _want(k_out, "k_out", torch.float16, shape, dev)
     if v_out is None:
-        v_out = torch.empty(shape, dtype=torch.float16, device=dev)
+        v_out = torch.empty_like(k_out)
     else:
         _want(v_out, "v_out", torch.float16, shape, dev)
     _call("apex_kv4_gather", index, kv_cache.data_ptr(), slot_mapping.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
@@ -230,16 +259,14 @@ def attention(q, kv_cache, block_table, context_lens, scale, out=None, lse_out=N
     from torch.zeros); calls that can overlap, and a captured graph, need one
     of their own."""
     torch = _torch()
-    nb, Hkv, dev, index = _cache(kv_cache)
-    B, stride = _batch(block_table, context_lens, dev)
-    Hq = _queries(q, B, Hkv, dev)
+    B, Hq, nb, Hkv, stride, index = _step(q, kv_cache, block_table, context_lens)
     if out is None:
-        out = torch.empty((B, Hq, HEAD_DIM), dtype=torch.float16, device=dev)
+        out = torch.empty_like(q)
     else:
-        _want(out, "out", torch.float16, q.shape, dev)
+        _want(out, "out", torch.float16, q.shape, q.device)
     if lse_out is not None:
-        _want(lse_out, "lse_out", torch.float32, (B, Hq), dev)
-    ws, ws_bytes = _workspace(workspace, dev)
+        _want(lse_out, "lse_out", torch.float32, (B, Hq), q.device)
+    ws, ws_bytes = (None, 0) if workspace is None else _workspace(workspace, q.device)
     _call("apex_kv4_attention", index, q.data_ptr(), kv_cache.data_ptr(), block_table.data_ptr(), stride,
           context_lens.data_ptr(), out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), B, Hq, Hkv,
           HEAD_DIM, BLOCK_SIZE, nb, scale, ws, ws_bytes, _raw_stream(stream, index))
@@ -250,9 +277,8 @@ def accumulate_weights(q, kv_cache, block_table, context_lens, scale, lse, weigh
     """apex_kv4_accumulate_weights over torch tensors (in place on ``weights``);
     ``lse`` fp32 [B][Hq] is the ``lse_out`` of the step's attention."""
     torch = _torch()
-    nb, Hkv, dev, index = _cache(kv_cache)
-    B, stride = _batch(block_table, context_lens, dev)
-    Hq = _queries(q, B, Hkv, dev)
+    B, Hq, nb, Hkv, stride, index = _step(q, kv_cache, block_table, context_lens)
+    dev = q.device
     _want(lse, "lse", torch.float32, (B, Hq), dev)
     _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev)
     _call("apex_kv4_accumulate_weights", index, q.data_ptr(), kv_cache.data_ptr(), block_table.data_ptr(), stride,
@@ -274,7 +300,7 @@ def evict(kv_cache, block_table, context_lens, weights, positions, keep, sinks=0
     B, stride = _batch(block_table, context_lens, dev)
     _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev)
     _want(positions, "positions", torch.int32, (nb, Hkv, BLOCK_SIZE), dev)
-    ws, ws_bytes = _workspace(workspace, dev)
+    ws, ws_bytes = (None, 0) if workspace is None else _workspace(workspace, dev)
     _call("apex_kv4_evict", index, kv_cache.data_ptr(), block_table.data_ptr(), stride, context_lens.data_ptr(),
           weights.data_ptr(), positions.data_ptr(), B, Hkv, HEAD_DIM, BLOCK_SIZE, nb, keep, sinks, recent, ws, ws_bytes,
           _raw_stream(stream, index))
