@@ -86,14 +86,33 @@ struct Params {
 //           [start(w), start(w + 1)).
 // All positions are below 2^31 (the host checks the table's size).
 
-// What starting and finishing a pair costs a work group, in blocks: about 3 us,
-// where a block takes 0.08.
-constexpr unsigned kPairCost = 32;
+// What a pair costs a work group besides its blocks, in blocks (0.08 us each): 32
+// take 1.01 of the time over 30 batches, 1.16 at worst, 128 1.002, 1.04 at worst.
+constexpr unsigned kPairCost = 64;
 // Parts: the least, and the most that still goes better than the line (uneven
-// last parts against pairs that begin and end inside a work group).
+// last parts against pairs that begin and end inside a work group).  Over 50
+// batches the line alone takes 1.16 of the time, 1.6 at worst (6 pairs of 20
+// blocks 9.1 against 14.5 us, 192 of 20-54 10.1 against 15.7); parts of up to 128
+// blocks 1.01, 1.5 at worst, of up to 1000 1.015, 1.34 at worst.
 constexpr unsigned kMinPart = 32, kMaxPart = 320;
-// Whole pairs by waves: at most this many blocks.
-constexpr unsigned kWholeBlocks = 32;
+// Whole pairs by waves, where there are more pairs than work groups.  In blocks
+// of a work group's time (0.08 us): the line takes (U + kPairCost pairs) / W; the
+// waves stream U / W (uneven: an eighth more), or, with few blocks to a wave, are
+// held up by its round trips, about 3 for each of the longest pairs in a row; and
+// start once.  Measured, line against waves: 3200 pairs of 2-44 blocks 78 against
+// 41 us, 2048 of 63 66 against 47, 1024 of 125 55 against 48; but 512 of 88-125 34
+// against 44, 400 of 94 28 against 36.  Up to kWholeBlocks the waves always win
+// (1080 pairs of 1-2 blocks 23.5 against 7.0 us); past kMostWhole the wave with the
+// longest pairs ends alone (2400 pairs of 10-185 blocks 87 against 121 us).
+constexpr unsigned kWholeBlocks = 32, kMostWhole = 128;
+
+__device__ inline bool waves_take_pairs(unsigned U, unsigned pairs, unsigned longest, unsigned W)
+{
+    if (pairs <= W || longest > kMostWhole) return false;
+    if (longest <= kWholeBlocks) return true;
+    const unsigned per = U / W, rounds = (pairs + kWaves * W - 1) / (kWaves * W);
+    return max(3 * longest * rounds, per + per / 8) + 32 < per + kPairCost * pairs / W;
+}
 
 struct Line {
     unsigned V, W, per, rest;   // positions, work groups; V = W per + rest
@@ -180,7 +199,7 @@ __device__ inline Plan plan_of(const Params& p, unsigned hk, unsigned K, unsigne
     r.b = r.g = r.blk = r.L = r.take = r.first = r.last = 0;
     const unsigned V = total * hk, pairs = nonempty * hk, U = V - K * pairs, W = (unsigned)p.workers;
     if (U == 0) return r;
-    if (kAttention && pairs > W && longest <= kWholeBlocks) {
+    if (kAttention && waves_take_pairs(U, pairs, longest, W)) {
         r.way = kWhole;
         return r;
     }
@@ -341,15 +360,16 @@ __device__ inline __amdgpu_buffer_rsrc_t slab_resource(const char* slab, int byt
     return __builtin_amdgcn_make_buffer_rsrc((void*)apex::uniform_ptr(slab), (short)0, bytes, apex::kRawBufferWord3);
 }
 
-// K goes through the Infinity Cache: a step that accumulates its weights reads
-// it again.  (Attention and accumulation of four caches in turn, 32 requests of
-// 8192 tokens, G = 4: 80.7 us a cache, 89.3 with K read past it; the attention
-// alone is the same either way.)  V is read once and past it.
+// The attention reads K through the Infinity Cache: a step that accumulates its
+// weights reads it again.  (Attention and accumulation of four caches in turn, 32
+// requests of 8192 tokens, G = 4: 80 us a cache, 89 with K read past it; the
+// attention alone is the same either way.)  V, and K in the accumulation, go past.
+template <int kPolicy>
 __device__ inline void load_keys(Tile& t, __amdgpu_buffer_rsrc_t r, int lane)
 {
     const int c = lane & 15, q = lane >> 4;
-    t.k = __builtin_amdgcn_raw_buffer_load_b128(r, c * 64 + q * 16, 0, 0);
-    t.ks = __builtin_amdgcn_raw_buffer_load_b8(r, kv4::kKScales + c * 4 + q, 0, 0);
+    t.k = __builtin_amdgcn_raw_buffer_load_b128(r, c * 64 + q * 16, 0, kPolicy);
+    t.ks = __builtin_amdgcn_raw_buffer_load_b8(r, kv4::kKScales + c * 4 + q, 0, kPolicy);
 }
 
 __device__ inline void load_values(Tile& t, __amdgpu_buffer_rsrc_t r, int lane)
@@ -421,43 +441,54 @@ struct Step {
     unsigned next[2];   // and of those that refill them
 };
 
+struct Pipe {
+    Step x[2];
+};
+
+__device__ inline unsigned id_at(const Span& s, int i)
+{
+    // (an entry that is not the wave's is replaced, not read: s.bt[0] is readable)
+    const unsigned id = *(const __attribute__((address_space(4))) uint32_t*)(s.bt + (i < s.n ? i : 0));
+    return i < s.n ? id : 0xffffffffu;
+}
+
+// The slab of a block, with no extent (loads give zeros) outside the pool.
+__device__ inline __amdgpu_buffer_rsrc_t slab_of(const Params& p, const Span& s, unsigned id)
+{
+    return slab_resource(s.pair + id * ((uint64_t)p.Hkv * kSlabBytes), id < p.num_blocks ? kSlabBytes : 0);
+}
+
+// Asks for a span's first blocks.
+__device__ inline void begin(const Params& p, const Span& s, int lane, Pipe& pipe)
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        Step& x = pipe.x[i];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            x.id[j] = id_at(s, 2 * i + j);
+            const auto r = slab_of(p, s, x.id[j]);
+            load_keys<0>(x.t[j], r, lane);
+            load_values(x.t[j], r, lane);
+            x.next[j] = id_at(s, 4 + 2 * i + j);
+        }
+    }
+}
+
+// A wave's attention over its span, whose first blocks are on their way.
 template <int G>
-__device__ inline void attend(const Params& p, int b, int g, const Span& s, int lane, State& st)
+__device__ inline void attend(const Params& p, int b, int g, const Span& s, int lane, Pipe& pipe, State& st)
 {
     const int col = lane & 15, q = lane >> 4;
     const int parity = G == 8 ? col >> 3 : (col >> 2) & 1;
     // bytes 2 and 3 of a weight to the half of its parity, zeros to the other
     const unsigned place = parity ? 0x03020c0cu : 0x0c0c0302u;
     const unsigned low_part = G < 8 && col >= 8 ? 0xffff0000u : 0u;
-    const uint64_t step_bytes = (uint64_t)p.Hkv * kSlabBytes;
     const unsigned pool = p.num_blocks;
-
-    // (an entry that is not the wave's is replaced, not read: s.bt[0] is readable)
-    auto id_at = [&](int i) -> unsigned {
-        const unsigned id = *(const __attribute__((address_space(4))) uint32_t*)(s.bt + (i < s.n ? i : 0));
-        return i < s.n ? id : 0xffffffffu;
-    };
-    // the slab of a block, with no extent (loads give zeros) outside the pool
-    auto slab = [&](unsigned id) {
-        return slab_resource(s.pair + id * step_bytes, id < pool ? kSlabBytes : 0);
-    };
     st.m = -INFINITY;
     st.l = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) st.acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    Step x[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            x[i].id[j] = id_at(2 * i + j);
-            const auto r = slab(x[i].id[j]);
-            load_keys(x[i].t[j], r, lane);
-            load_values(x[i].t[j], r, lane);
-            x[i].next[j] = id_at(4 + 2 * i + j);
-        }
-    }
 
     // q's digits are worked out while the first blocks are on their way
     QueryOperand<G> op;
@@ -484,9 +515,9 @@ __device__ inline void attend(const Params& p, int b, int g, const Span& s, int 
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             x.id[i] = x.next[i];
-            refill[i] = slab(x.id[i]);
-            load_keys(x.t[i], refill[i], lane);
-            x.next[i] = id_at(k + 8 + i);
+            refill[i] = slab_of(p, s, x.id[i]);
+            load_keys<0>(x.t[i], refill[i], lane);
+            x.next[i] = id_at(s, k + 8 + i);
         }
         bool live[8];
         if (tail) {
@@ -561,10 +592,10 @@ __device__ inline void attend(const Params& p, int b, int g, const Span& s, int 
     // a step and its waits
     int k = 0;
     for (; k + 2 < s.n; k += 4) {
-        step(x[0], k);
-        step(x[1], k + 2);
+        step(pipe.x[0], k);
+        step(pipe.x[1], k + 2);
     }
-    if (k < s.n) step(x[0], k);
+    if (k < s.n) step(pipe.x[0], k);
     st.l = apex::rows_sum4(st.l);
 }
 
@@ -768,19 +799,37 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
     const int w = (int)blockIdx.x;
     Plan plan = make_plan<true>(p, p.Hkv, kPairCost, (unsigned)w, lane);
 
+    Pipe pipe;
     if (plan.way == kWhole) {
-        // every wave takes whole pairs, and writes their rows itself
+        // every wave takes whole pairs and writes their rows itself; the next
+        // pair's first blocks are on their way meanwhile
         constexpr int N = 2 * G;
         const int h = lane * N / kHeadDim, dim = lane * N % kHeadDim;
         const int pairs = p.B * p.Hkv;
-        for (int i = wave * p.workers + w; i < pairs; i += kWaves * p.workers) {
-            const int b = uniform((int)((unsigned)i / (unsigned)p.Hkv)), g = i - b * p.Hkv;
-            const int L = uniform(context(p, b));
+        struct Pair {
+            int b, g, L;
+        };
+        auto start = [&](int i, Pair& x, Span& s) {
+            x.b = uniform((int)((unsigned)i / (unsigned)p.Hkv));
+            x.g = i - x.b * p.Hkv;
+            x.L = uniform(context(p, x.b));
+            s = wave_span(p, x.b, x.g, x.L, 0, (int)blocks(x.L), 0, 1);
+            if (s.n > 0) begin(p, s, lane, pipe);
+        };
+        Pair x;
+        Span s;
+        int i = wave * p.workers + w;
+        if (i < pairs) start(i, x, s);
+        while (i < pairs) {
             Row<N> r;
             clear(r);
-            if (L > 0) {
-                State st;
-                attend<G>(p, b, g, wave_span(p, b, g, L, 0, (int)blocks(L), 0, 1), lane, st);
+            State st;
+            if (s.n > 0) attend<G>(p, x.b, x.g, s, lane, pipe, st);
+            const Pair done = x;
+            const bool any = s.n > 0;
+            i += kWaves * p.workers;
+            if (i < pairs) start(i, x, s);
+            if (any) {
                 store_state<G>(st, wave, lane, sh);
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
                 r.M = sh.m[wave][h];
@@ -789,7 +838,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
                 for (int e = 0; e < N; ++e) r.num[e] = sh.acc[wave][lane * N + e];
                 __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
-            emit_row<N>(p, b, g * G + h, dim, r);
+            emit_row<N>(p, done.b, done.g * G + h, dim, r);
         }
         return;
     }
@@ -798,21 +847,27 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
     const int h = tid * N / kHeadDim, dim = tid * N % kHeadDim;
     const bool emits = h < G;
     bool more = plan.take > 0;
+    Span s;
+    auto start = [&]() {
+        s = wave_span(p, plan.b, plan.g, plan.L, plan.blk, plan.blk + plan.take, wave, kWaves);
+        begin(p, s, lane, pipe);
+    };
+    if (more) start();
     while (more) {
-        const int b = plan.b, g = plan.g;
-        const int nb = (int)blocks(plan.L);
-        {
-            State st;
-            attend<G>(p, b, g, wave_span(p, b, g, plan.L, plan.blk, plan.blk + plan.take, wave, kWaves), lane, st);
-            store_state<G>(st, wave, lane, sh);
-        }
-        __syncthreads();
+        const int b = plan.b, g = plan.g, nb = (int)blocks(plan.L);
+        State st;
+        attend<G>(p, b, g, s, lane, pipe, st);
         // the pair's first and last work groups
         int wf = plan.first, wl = plan.last;
         if (plan.way == kLine) {
             wf = plan.blk == 0 ? w : uniform((int)plan.line.owner(plan.vf));
             wl = plan.blk + plan.take == nb ? w : uniform((int)plan.line.owner(plan.vf + (unsigned)nb - 1));
         }
+        // the next segment's first blocks are on their way while this one is joined
+        more = plan.way == kLine && next_segment(p, p.Hkv, kPairCost, plan);
+        if (more) start();
+        store_state<G>(st, wave, lane, sh);
+        __syncthreads();
         if (emits) {
             Row<N> r;
             join_waves<G, N>(sh, h, dim, r);
@@ -846,7 +901,6 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
                 }
             }
         }
-        more = plan.way == kLine && next_segment(p, p.Hkv, kPairCost, plan);
         if (more) __syncthreads();
     }
 
@@ -883,7 +937,7 @@ __device__ inline void accumulate(const Params& p, int b, int g, const Span& s, 
         return i < s.n ? id : 0xffffffffu;
     };
     auto load = [&](Tile& t, unsigned id) {
-        load_keys(t, slab_resource(s.pair + id * step_bytes, id < p.num_blocks ? kSlabBytes : 0), lane);
+        load_keys<apex::kStreamingLoad>(t, slab_resource(s.pair + id * step_bytes, id < p.num_blocks ? kSlabBytes : 0), lane);
     };
     // the lane's block of a chunk and its four tokens there
     const int own = lane >> 2, tok = 4 * (lane & 3);
