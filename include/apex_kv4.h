@@ -89,11 +89,11 @@ int apex_kv4_gather(const void* kv_cache, const int64_t* slot_mapping, void* k_o
  * a row of q that holds a NaN or an infinity gives NaNs, a result past 65504
  * (of values that an append rounded up) is 65504.
  * workspace: device memory of apex_kv4_attention_workspace_bytes bytes, 256-byte
- * aligned, whose first apex_kv4_attention_counter_bytes bytes are zero (every
- * call leaves them zero again), or NULL for the library's own, one per device,
- * grown on demand (growing waits for the device).  Calls that can overlap need
- * a workspace each, and so do a captured graph's calls: under stream capture
- * NULL is refused.
+ * aligned, all zero before its first call (calls of any shapes that it is large
+ * enough for may follow; what they need zero they leave zero), or NULL for the
+ * library's own, one per device, grown on demand (growing waits for the device).
+ * Calls that can overlap need a workspace each, and so do a captured graph's
+ * calls: under stream capture NULL is refused.
  */
 int apex_kv4_attention(const void* q, const void* kv_cache, const int32_t* block_table,
                        int64_t block_table_stride, const int32_t* context_lens, void* out, float* lse_out,
@@ -102,13 +102,12 @@ int apex_kv4_attention(const void* q, const void* kv_cache, const int32_t* block
 
 /* 0 on bad shapes. */
 size_t apex_kv4_attention_workspace_bytes(int B, int Hq, int Hkv);
-size_t apex_kv4_attention_counter_bytes(int B, int Hkv);
 
 /*
  * Accumulates the attention weights of a step whose log-sum-exp is lse:
  *     weights[slot of t][g] += sum over h of kv-head g of exp(scale * q[b][h] . K_t - lse[b][h]),  t in [0, L_b)
  * (the weights that the step's softmax gave the token, over the q-heads of its
- * kv-head).  No block may belong to two requests of one call.
+ * kv-head).  A block may occur only once in the call's table rows.
  */
 int apex_kv4_accumulate_weights(const void* q, const void* kv_cache, const int32_t* block_table,
                                 int64_t block_table_stride, const int32_t* context_lens, const float* lse,
@@ -128,7 +127,7 @@ int apex_kv4_accumulate_weights(const void* q, const void* kv_cache, const int32
  * takes the i-th kept token from [keep, L_b), both counted upwards: its K and V
  * row, weight and position.  Slots from keep on are left as they are.  (The
  * attention does not depend on the order of the cached tokens; positions keeps
- * track of it.)  No block may belong to two requests of one call.
+ * track of it.)  A block may occur only once in the call's table rows.
  * workspace: apex_kv4_evict_workspace_bytes bytes, 256-byte aligned, any content,
  * or NULL as above.
  */

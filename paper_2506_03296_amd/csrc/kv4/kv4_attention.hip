@@ -1012,16 +1012,16 @@ __global__ __launch_bounds__(kWeightThreads, 3) void weights_kernel(Params p)
 
 // --- host -------------------------------------------------------------------------
 
+// A workspace: the partials at the size of the widest group, then the arrival
+// counters, so that calls of any shapes find the counters where no call leaves
+// partials.
 size_t counter_bytes(int B, int Hkv) { return kv4::align_up((size_t)B * Hkv * sizeof(int32_t), 256); }
 
-size_t acc_bytes(int workers, int G)
-{
-    return kv4::align_up(sizeof(float) * 2 * (size_t)workers * G * kHeadDim, 256);
-}
+size_t acc_bytes(int workers) { return kv4::align_up(sizeof(float) * 2 * (size_t)workers * 8 * kHeadDim, 256); }
 
-size_t partial_bytes(int workers, int G)
+size_t partial_bytes(int workers)
 {
-    return acc_bytes(workers, G) + kv4::align_up(sizeof(float) * 4 * (size_t)workers * G, 256);
+    return acc_bytes(workers) + kv4::align_up(sizeof(float) * 4 * (size_t)workers * 8, 256);
 }
 
 template <typename F>
@@ -1035,9 +1035,12 @@ void with_group(int G, F f)
     }
 }
 
-int check_pointers(const void* q, const void* cache, const void* bt, const void* lens, const void* more, const char* name)
+// (an empty pool or table may be NULL)
+int check_pointers(const void* q, const void* cache, int64_t num_blocks, const void* bt, int64_t stride, const void* lens,
+                   const void* more, const char* name)
 {
-    if (!q || !cache || !bt || !lens || !more) return fail(APEX_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if (!q || (!cache && num_blocks > 0) || (!bt && stride > 0) || !lens || !more)
+        return fail(APEX_ERR_INVALID_ARG, "a tensor pointer is NULL");
     if (!kv4::aligned(q, 16) || !kv4::aligned(cache, 16))
         return fail(APEX_ERR_INVALID_ARG, "q and kv_cache must be 16-byte aligned");
     if (!kv4::aligned(bt, 4) || !kv4::aligned(lens, 4))
@@ -1069,23 +1072,13 @@ Params fill(const void* q, const void* cache, const int32_t* bt, int64_t stride,
 
 extern "C" {
 
-size_t apex_kv4_attention_counter_bytes(int B, int Hkv)
-{
-    apex::clear_error();
-    if (B < 0 || Hkv <= 0) {
-        fail(APEX_ERR_INVALID_ARG, "B = %d or Hkv = %d", B, Hkv);
-        return 0;
-    }
-    return counter_bytes(B, Hkv);
-}
-
 size_t apex_kv4_attention_workspace_bytes(int B, int Hq, int Hkv)
 {
     apex::clear_error();
     int cus = 0;
     if (kv4::check_batch(B, Hq, Hkv, kHeadDim, kBlockSize, 0, 0) != APEX_OK || kv4::compute_units(&cus) != APEX_OK)
         return 0;
-    return counter_bytes(B, Hkv) + partial_bytes(cus, Hq / Hkv);
+    return partial_bytes(cus) + counter_bytes(B, Hkv);
 }
 
 int apex_kv4_attention(const void* q, const void* kv_cache, const int32_t* block_table, int64_t block_table_stride,
@@ -1096,7 +1089,7 @@ int apex_kv4_attention(const void* q, const void* kv_cache, const int32_t* block
     apex::clear_error();
     int rc = kv4::check_batch(B, Hq, Hkv, d, block_size, num_blocks, block_table_stride);
     if (rc != APEX_OK || B == 0) return rc;
-    rc = check_pointers(q, kv_cache, block_table, context_lens, out, "out");
+    rc = check_pointers(q, kv_cache, num_blocks, block_table, block_table_stride, context_lens, out, "out");
     if (rc != APEX_OK) return rc;
     if (!kv4::aligned(lse_out, 4)) return fail(APEX_ERR_INVALID_ARG, "lse_out must be 4-byte aligned");
     const size_t qo = (size_t)B * Hq * d * 2;
@@ -1113,11 +1106,10 @@ int apex_kv4_attention(const void* q, const void* kv_cache, const int32_t* block
     int cus = 0;
     rc = kv4::compute_units(&cus);
     if (rc != APEX_OK) return rc;
-    const int G = Hq / Hkv;
-    const size_t cb = counter_bytes(B, Hkv), pb = partial_bytes(cus, G);
-    void *counters = workspace, *partials = (char*)workspace + cb;
+    const size_t cb = counter_bytes(B, Hkv), pb = partial_bytes(cus);
+    void *partials = workspace, *counters = (char*)workspace + pb;
     if (workspace) {
-        rc = kv4::check_workspace(workspace, workspace_bytes, cb + pb);
+        rc = kv4::check_workspace(workspace, workspace_bytes, pb + cb);
     } else {
         rc = kv4::library_buffer(kv4::kCounters, cb, (hipStream_t)stream, &counters);
         if (rc == APEX_OK) rc = kv4::library_buffer(kv4::kPartials, pb, (hipStream_t)stream, &partials);
@@ -1128,8 +1120,8 @@ int apex_kv4_attention(const void* q, const void* kv_cache, const int32_t* block
     p.lse = lse_out;
     p.counters = (int32_t*)counters;
     p.pacc = (float*)partials;
-    p.pml = (float*)((char*)partials + acc_bytes(cus, G));
-    with_group(G, [&](auto g) {
+    p.pml = (float*)((char*)partials + acc_bytes(cus));
+    with_group(Hq / Hkv, [&](auto g) {
         attention_kernel<decltype(g)::value><<<(unsigned)cus, kThreads, 0, (hipStream_t)stream>>>(p);
     });
     return kv4::launched("kv4 attention");
@@ -1143,7 +1135,8 @@ int apex_kv4_accumulate_weights(const void* q, const void* kv_cache, const int32
     apex::clear_error();
     int rc = kv4::check_batch(B, Hq, Hkv, d, block_size, num_blocks, block_table_stride);
     if (rc != APEX_OK || B == 0) return rc;
-    rc = check_pointers(q, kv_cache, block_table, context_lens, weights, "weights");
+    if (num_blocks == 0) return APEX_OK;   // no token is in the pool
+    rc = check_pointers(q, kv_cache, num_blocks, block_table, block_table_stride, context_lens, weights, "weights");
     if (rc != APEX_OK) return rc;
     if (!lse) return fail(APEX_ERR_INVALID_ARG, "a tensor pointer is NULL");
     if (!kv4::aligned(lse, 4)) return fail(APEX_ERR_INVALID_ARG, "lse must be 4-byte aligned");

@@ -467,7 +467,9 @@ extern "C" int apex_kv4_evict(void* kv_cache, const int32_t* block_table, int64_
         return fail(APEX_ERR_INVALID_ARG, "keep = %d, sinks = %d, recent = %d: keep must be positive, sinks + recent at most keep",
                     keep, sinks, recent);
     if ((int64_t)B * Hkv >= 1 << 22) return fail(APEX_ERR_UNSUPPORTED, "B * Hkv = %lld reaches 2^22", (long long)B * Hkv);
-    if (B == 0) return APEX_OK;
+    // no request can be longer than keep, no token is in the pool
+    const int64_t longest = block_table_stride * kBlockSize;
+    if (B == 0 || longest <= keep || num_blocks == 0) return APEX_OK;
     if (!kv_cache || !block_table || !context_lens || !weights || !positions)
         return fail(APEX_ERR_INVALID_ARG, "a tensor pointer is NULL");
     if (!aligned(kv_cache, 16) || !aligned(weights, 16))
@@ -487,8 +489,6 @@ extern "C" int apex_kv4_evict(void* kv_cache, const int32_t* block_table, int64_
     rc = workspace ? check_workspace(workspace, workspace_bytes, need)
                    : library_buffer(kMasks, need, (hipStream_t)stream, &workspace);
     if (rc != APEX_OK) return rc;
-    const int64_t longest = block_table_stride * kBlockSize;
-    if (longest <= keep || num_blocks == 0) return APEX_OK;   // no request can be longer, no token is in the pool
     int cus = 0;
     rc = compute_units(&cus);
     if (rc != APEX_OK) return rc;

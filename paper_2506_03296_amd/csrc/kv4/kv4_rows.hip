@@ -220,7 +220,7 @@ extern "C" int apex_kv4_append(const void* k_new, const void* v_new, int64_t new
                     (long long)new_token_stride);
     if ((positions != nullptr) != (token_positions != nullptr))
         return fail(APEX_ERR_INVALID_ARG, "positions and token_positions go together");
-    if (T == 0) return APEX_OK;
+    if (T == 0 || num_blocks == 0) return APEX_OK;   // no row, or every slot is out of the pool
     if (!k_new || !v_new || !kv_cache || !slot_mapping) return fail(APEX_ERR_INVALID_ARG, "a tensor pointer is NULL");
     if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(kv_cache, 16) || !aligned(weights, 16))
         return fail(APEX_ERR_INVALID_ARG, "k_new, v_new, kv_cache and weights must be 16-byte aligned");
@@ -237,7 +237,6 @@ extern "C" int apex_kv4_append(const void* k_new, const void* v_new, int64_t new
     if ((rc = check_disjoint(in[4], in, 4)) != APEX_OK || (rc = check_disjoint(in[5], in, 5)) != APEX_OK ||
         (rc = check_disjoint(in[6], in, 6)) != APEX_OK)
         return rc;
-    if (num_blocks == 0) return APEX_OK;   // every slot is out of the pool
     const RowShape s = {T, Hkv, num_blocks * kBlockSize, stride * 2};
     const auto kernel = 2 * (size_t)T * row * 2 > kCachedBytes ? append_kernel<true> : append_kernel<false>;
     kernel<<<row_grid(T, Hkv), kThreads, 0, (hipStream_t)stream>>>(
@@ -252,7 +251,7 @@ extern "C" int apex_kv4_gather(const void* kv_cache, const int64_t* slot_mapping
     int rc = check_cache(Hkv, d, block_size, num_blocks);
     if (rc == APEX_OK) rc = check_rows(T, Hkv);
     if (rc != APEX_OK || T == 0) return rc;
-    if (!kv_cache || !slot_mapping || !k_out || !v_out) return fail(APEX_ERR_INVALID_ARG, "a tensor pointer is NULL");
+    if ((!kv_cache && num_blocks > 0) || !slot_mapping || !k_out || !v_out) return fail(APEX_ERR_INVALID_ARG, "a tensor pointer is NULL");
     if (!aligned(k_out, 16) || !aligned(v_out, 16) || !aligned(kv_cache, 16))
         return fail(APEX_ERR_INVALID_ARG, "kv_cache, k_out and v_out must be 16-byte aligned");
     if (!aligned(slot_mapping, 8)) return fail(APEX_ERR_INVALID_ARG, "slot_mapping must be 8-byte aligned");

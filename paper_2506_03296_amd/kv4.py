@@ -21,13 +21,13 @@ from . import APEX_ERR_HIP, APEX_OK, ApexError, _on, _raw_stream, _require, _tor
 
 __all__ = ["LIB_PATH", "EXPORTED_SYMBOLS", "SLAB_BYTES", "BLOCK_SIZE", "HEAD_DIM", "load_library", "last_error",
            "empty_cache", "append", "gather", "attention", "accumulate_weights", "evict",
-           "attention_workspace_bytes", "attention_counter_bytes", "evict_workspace_bytes", "release_workspace"]
+           "attention_workspace_bytes", "evict_workspace_bytes", "release_workspace"]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libapex_kv4.so")
 EXPORTED_SYMBOLS = (
     "apex_kv4_append", "apex_kv4_gather", "apex_kv4_attention", "apex_kv4_attention_workspace_bytes",
-    "apex_kv4_attention_counter_bytes", "apex_kv4_accumulate_weights", "apex_kv4_evict",
-    "apex_kv4_evict_workspace_bytes", "apex_kv4_last_error", "apex_kv4_release_workspace",
+    "apex_kv4_accumulate_weights", "apex_kv4_evict", "apex_kv4_evict_workspace_bytes",
+    "apex_kv4_last_error", "apex_kv4_release_workspace",
 )
 SLAB_BYTES = 2176
 BLOCK_SIZE = 16
@@ -56,7 +56,6 @@ def load_library(path=None):
             ("apex_kv4_gather", i32, [vp, vp, vp, vp, i32, i32, i32, i32, i64, vp]),
             ("apex_kv4_attention", i32, [vp, vp, vp, i64, vp, vp, vp, i32, i32, i32, i32, i32, i64, f32, vp, size, vp]),
             ("apex_kv4_attention_workspace_bytes", size, [i32, i32, i32]),
-            ("apex_kv4_attention_counter_bytes", size, [i32, i32]),
             ("apex_kv4_accumulate_weights", i32, [vp, vp, vp, i64, vp, vp, vp, i32, i32, i32, i32, i32, i64, f32, vp]),
             ("apex_kv4_evict", i32, [vp, vp, i64, vp, vp, vp, i32, i32, i32, i32, i64, i32, i32, i32, vp, size, vp]),
             ("apex_kv4_evict_workspace_bytes", size, [i32, i32, i64]),
@@ -98,10 +97,6 @@ def release_workspace():
 def attention_workspace_bytes(B, Hq, Hkv):
     """Bytes of an attention workspace on the current device (0: bad shapes)."""
     return int(load_library().apex_kv4_attention_workspace_bytes(B, Hq, Hkv))
-
-
-def attention_counter_bytes(B, Hkv):
-    return int(load_library().apex_kv4_attention_counter_bytes(B, Hkv))
 
 
 def evict_workspace_bytes(B, Hkv, block_table_stride):
@@ -213,8 +208,8 @@ def append(k_new, v_new, kv_cache, slot_mapping, token_positions=None, positions
     ks, vs = k_new.stride(), v_new.stride()
     if ks[2] != 1 or vs[2] != 1 or (Hkv > 1 and (ks[1] != HEAD_DIM or vs[1] != HEAD_DIM)):
         raise ValueError("each token's rows must be contiguous [Hkv][d]")
-    if T > 1 and ks[0] != vs[0]:
-        raise ValueError("k_new and v_new must share the token stride")
+    if T > 1 and (ks[0] != vs[0] or ks[0] < Hkv * HEAD_DIM):
+        raise ValueError("k_new and v_new must share the token stride, at least Hkv * d")
     _want(slot_mapping, "slot_mapping", torch.int64, (T,), dev)
     if (positions is None) != (token_positions is None):
         raise ValueError("positions and token_positions go together")
@@ -255,9 +250,8 @@ def attention(q, kv_cache, block_table, context_lens, scale, out=None, lse_out=N
     """apex_kv4_attention over torch tensors; returns ``out``.
 
     ``workspace`` is an optional uint8 tensor of attention_workspace_bytes(B,
-    Hq, Hkv) bytes whose first attention_counter_bytes(B, Hkv) are zero (e.g.
-    from torch.zeros); calls that can overlap, and a captured graph, need one
-    of their own."""
+    Hq, Hkv) bytes or more, made by torch.zeros (calls of other shapes may share
+    it); calls that can overlap, and a captured graph, need one of their own."""
     torch = _torch()
     B, Hq, nb, Hkv, stride, index = _step(q, kv_cache, block_table, context_lens)
     if out is None:
@@ -296,6 +290,9 @@ def evict(kv_cache, block_table, context_lens, weights, positions, keep, sinks=0
     block_table.shape[1]) bytes; calls that can overlap, and a captured graph,
     need one of their own."""
     torch = _torch()
+    if not (0 < keep < 1 << 31 and sinks >= 0 and recent >= 0 and sinks + recent <= keep):
+        raise ValueError(f"keep = {keep}, sinks = {sinks}, recent = {recent}: keep must be positive (below 2^31), "
+                         "sinks + recent at most keep")
     nb, Hkv, dev, index = _cache(kv_cache)
     B, stride = _batch(block_table, context_lens, dev)
     _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev)

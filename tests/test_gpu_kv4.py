@@ -578,7 +578,37 @@ def test_two_streams_with_a_workspace_each(torch, kv4):
             kv4.attention(dq, dc, dt, dl, 0.1, out=out, workspace=ws, stream=s)
     torch.cuda.synchronize()
     assert all(torch.equal(out, want) for _, _, out in runs)
-    assert not any(ws[:kv4.attention_counter_bytes(4, 2)].any() for _, ws, _ in runs)
+
+
+def test_one_workspace_for_calls_of_many_shapes(torch, kv4):
+    """Partials of one call lie where no other call looks for its counters."""
+    ws = torch.zeros(kv4.attention_workspace_bytes(700, 8, 8), dtype=torch.uint8, device="cuda")
+    for lens, Hq, Hkv in (([3000], 8, 1), ([40] * 700, 8, 8), ([2000, 5, 900], 4, 4), ([1500] * 40, 8, 4), ([9000], 2, 1),
+                          ([3000], 8, 1)):
+        q, cache, table, lens = case(lens, Hq, Hkv, seed=len(lens) + Hq)
+        dq, dc, dt, dl = dev(torch, q, cache, table, lens)
+        own = torch.zeros(kv4.attention_workspace_bytes(len(lens), Hq, Hkv), dtype=torch.uint8, device="cuda")
+        for _ in range(2):
+            assert torch.equal(kv4.attention(dq, dc, dt, dl, 0.1, workspace=ws), kv4.attention(dq, dc, dt, dl, 0.1, workspace=own))
+
+
+def test_empty_tables_and_pools(torch, kv4):
+    q = torch.randn((2, 4, D), device="cuda").half()
+    lens = torch.tensor([0, 5], dtype=torch.int32, device="cuda")
+    wide, none = (torch.zeros((2, n), dtype=torch.int32, device="cuda") for n in (3, 0))
+    lse = torch.zeros((2, 4), device="cuda")
+    for nb, table in ((3, none), (0, wide), (0, none)):
+        c = torch.full((nb, 2, SLAB), 255, dtype=torch.uint8, device="cuda")
+        out = kv4.attention(q, c, table, lens, 0.1, lse_out=lse)
+        assert not out.any() and torch.isinf(lse).all()
+        w, p = torch.ones((nb, 2, BS), device="cuda"), torch.zeros((nb, 2, BS), dtype=torch.int32, device="cuda")
+        kv4.accumulate_weights(q, c, table, lens, 0.1, lse, w)
+        kv4.evict(c, table, lens, w, p, 2)
+        assert (w == 1).all() and (c == 255).all()
+    k, v = kv4.gather(c, torch.tensor([0, -1, 70], device="cuda"))
+    assert not k.any() and not v.any()
+    kv4.append(torch.ones((2, 2, D), device="cuda").half(), torch.ones((2, 2, D), device="cuda").half(), c,
+               torch.tensor([0, 1], device="cuda"))
 
 
 def test_growing_and_releasing_the_librarys_workspace(torch, kv4):
@@ -647,6 +677,14 @@ def test_binding_pairs_of_arguments(torch, kv4):
         kv4.append(k, k[:, :1], c, s)
     with pytest.raises(ValueError):
         kv4.append(k, torch.zeros((5, 4, D), dtype=torch.float16, device="cuda")[:, :2], c, s)
+    with pytest.raises(ValueError):
+        kv4.append(k[:1].expand(5, 2, D), k[:1].expand(5, 2, D), c, s)     # no stride between tokens
+    b = torch.zeros((1, 3), dtype=torch.int32, device="cuda")
+    n = torch.full((1,), 40, dtype=torch.int32, device="cuda")
+    w, p = torch.zeros((3, 2, BS), device="cuda"), torch.zeros((3, 2, BS), dtype=torch.int32, device="cuda")
+    for budget in ((0,), (-1,), (1 << 32,), (8, -1), (8, 0, -1), (8, 5, 4)):
+        with pytest.raises(ValueError):
+            kv4.evict(c, b, n, w, p, *budget)
     kv4.append(k[:0], k[:0], c, s[:0])
     assert kv4.gather(c, s[:0])[0].shape == (0, 2, D)
     e = torch.empty((0, 4, D), dtype=torch.float16, device="cuda")

@@ -122,14 +122,15 @@ def test_nothing_to_do(lib):
     assert accumulate(lib, B=0, q=None, w=None) == A.APEX_OK
     assert evict(lib, B=0, cache=None) == A.APEX_OK
     assert append(lib, nb=0) == A.APEX_OK
+    assert accumulate(lib, nb=0) == A.APEX_OK
+    assert evict(lib, nb=0) == A.APEX_OK
+    assert evict(lib, stride=0, bt=None) == A.APEX_OK
     # no request can be longer than `keep`
     assert evict(lib, keep=160, ws=at(7), ws_bytes=1 << 30) == A.APEX_OK
     assert kv4.last_error() == ""
 
 
 def test_workspace_sizes(lib):
-    assert kv4.attention_counter_bytes(4, 8) == 256 and kv4.attention_counter_bytes(100, 8) == 3328
-    assert kv4.attention_counter_bytes(-1, 8) == 0
     assert kv4.evict_workspace_bytes(0, 8, 10) == 0
     # a count per pair and a bit per slot
     assert kv4.evict_workspace_bytes(4, 8, 10) == 256 + 32 * 3 * 8
