@@ -137,8 +137,7 @@ def evict(cache, table, lens, weights, positions, keep, sinks, recent):
         block, at = table[b][t // BS], t % BS
         for g in range(cache.shape[1]):
             kept = kept_tokens(weights[block, g, at], positions[block, g, at], keep, sinks, recent)
-            for to, src in zip(np.flatnonzero(~kept[:keep]), keep + np.flatnonzero(kept[keep:])):
-                for ot, of in zip(row_offsets(at[to]), row_offsets(at[src])):
-                    cache[block[to], g, ot] = cache[block[src], g, of]
-                weights[block[to], g, at[to]] = weights[block[src], g, at[src]]
-                positions[block[to], g, at[to]] = positions[block[src], g, at[src]]
+            to, src = np.flatnonzero(~kept[:keep]), keep + np.flatnonzero(kept[keep:])
+            cache[block[to][:, None], g, OFFSETS[at[to]]] = cache[block[src][:, None], g, OFFSETS[at[src]]]
+            weights[block[to], g, at[to]] = weights[block[src], g, at[src]]
+            positions[block[to], g, at[to]] = positions[block[src], g, at[src]]

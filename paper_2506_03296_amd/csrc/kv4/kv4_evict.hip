@@ -14,6 +14,8 @@
 // below `keep` takes the i-th kept one from `keep` on.  Sources and targets are
 // disjoint, so the moves need no order, and a cut by a few tokens moves a few
 // rows.
+#include <type_traits>
+
 #include "kv4_host.h"
 
 namespace {
@@ -78,7 +80,9 @@ __device__ inline int wave_scan(int x, int lane)
 template <int kN>
 struct Moves {
     int64_t to[kN], from[kN];   // slot indexes
+    int2 hole_words[kN], mover_words[kN];   // words with listed slots: index, rank of the first
     int holes[kN / 64], movers[kN / 64];
+    int hole_n, mover_n;
 };
 
 // Moves r0 .. r0 + kN of a pair's n, by kN threads.
@@ -88,24 +92,30 @@ __device__ inline void move_rows(const EvictParams& p, const int32_t* row, int g
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, keep = p.keep;
     // a thread counts the holes (evicted below keep) and movers (kept from keep
-    // on) of consecutive words, a scan ranks them, then it lists its own
+    // on) of consecutive words and a scan ranks them; the words with any of the
+    // kN looked for, at most kN, are put down, and a wave lists a word's slots, a
+    // lane each
     const int words = (L + 63) / 64, per = (words + kN - 1) / kN;
     const int a = min(words, tid * per), e = min(words, a + per);
-    auto below = [&](int w) -> uint64_t {   // bits of the word's slots below keep
+    auto hole_bits = [&](int w) -> uint64_t {
         const int left = keep - w * 64;
-        return left <= 0 ? 0ull : left >= 64 ? ~0ull : (1ull << left) - 1;
+        return ~kept[w] & (left <= 0 ? 0ull : left >= 64 ? ~0ull : (1ull << left) - 1);
+    };
+    auto mover_bits = [&](int w) -> uint64_t {
+        const int skip = keep - w * 64;
+        return kept[w] & (skip <= 0 ? ~0ull : skip >= 64 ? 0ull : ~0ull << skip);
     };
     int holes = 0, movers = 0;
     for (int w = a; w < e; ++w) {
-        const uint64_t k = kept[w], low = below(w);
-        holes += __popcll(~k & low);
-        movers += __popcll(k & ~low);
+        holes += __popcll(hole_bits(w));
+        movers += __popcll(mover_bits(w));
     }
     int hole = wave_scan(holes, lane), mover = wave_scan(movers, lane);
     if (lane == 63) {
         sh.holes[wave] = hole;
         sh.movers[wave] = mover;
     }
+    if (tid == 0) sh.hole_n = sh.mover_n = 0;
     sh.to[tid] = sh.from[tid] = -1;
     __syncthreads();
     for (int i = 0; i < wave; ++i) {
@@ -115,20 +125,23 @@ __device__ inline void move_rows(const EvictParams& p, const int32_t* row, int g
     hole -= holes + r0;
     mover -= movers + r0;
     for (int w = a; w < e; ++w) {
-        const uint64_t k = kept[w], low = below(w);
-        uint64_t m = ~k & low;
-        if (hole + __popcll(m) <= 0 || hole >= kN)
-            hole += __popcll(m);
-        else
-            for (; m; m &= m - 1, ++hole)
-                if (hole >= 0 && hole < kN) sh.to[hole] = w * 64 + __builtin_ctzll(m);
-        m = k & ~low;
-        if (mover + __popcll(m) <= 0 || mover >= kN)
-            mover += __popcll(m);
-        else
-            for (; m; m &= m - 1, ++mover)
-                if (mover >= 0 && mover < kN) sh.from[mover] = w * 64 + __builtin_ctzll(m);
+        const int h = __popcll(hole_bits(w)), m = __popcll(mover_bits(w));
+        if (h > 0 && hole < kN && hole + h > 0) sh.hole_words[atomicAdd(&sh.hole_n, 1)] = make_int2(w, hole);
+        if (m > 0 && mover < kN && mover + m > 0) sh.mover_words[atomicAdd(&sh.mover_n, 1)] = make_int2(w, mover);
+        hole += h;
+        mover += m;
     }
+    __syncthreads();
+    auto list = [&](const int2* from, int n, auto bits, int64_t* to) {
+        for (int i = wave; i < n; i += kN / 64) {
+            const int2 x = from[i];
+            const uint64_t m = bits(x.x);
+            const int rank = x.y + __popcll(m & ((1ull << lane) - 1));
+            if ((m >> lane & 1) && rank >= 0 && rank < kN) to[rank] = x.x * 64 + lane;
+        }
+    };
+    list(sh.hole_words, sh.hole_n, hole_bits, sh.to);
+    list(sh.mover_words, sh.mover_n, mover_bits, sh.from);
     __syncthreads();
     // slots to indexes, one pair a thread
     const int64_t to_slot = sh.to[tid], from_slot = sh.from[tid];
@@ -191,10 +204,16 @@ __global__ __launch_bounds__(kSmall) void move_kernel(EvictParams p)
 
 // --- selection --------------------------------------------------------------------
 
+template <int kT>
 struct Select {
-    unsigned bins[kBins];
+    // counts of a digit, in copies by the lane's number: weights have few leading
+    // digits, and additions to one address wait for each other.  (First digit of a
+    // pair of 4664 tokens: 6.3 us with one copy, 3.2 with four; but of 1056 tokens
+    // with 256 threads, who clear and add up the copies, 2.1 and 3.9.)
+    static constexpr int kCopies = kT == kLarge ? 2 : 1;
+    unsigned bins[kBins][kCopies];
     uint64_t few[kFew];
-    int wave[kLarge / 64];
+    int wave[kT / 64];
     unsigned digit;
     int above, count, few_n;
     uint64_t last;
@@ -248,8 +267,9 @@ struct Tokens {
 };
 
 template <int kT, int kN, bool kAgain>
-__device__ inline void select_pair(const EvictParams& p, const int32_t* row, int g, int L, uint64_t* out, Select& sh)
+__device__ inline void select_pair(const EvictParams& p, const int32_t* row, int g, int L, uint64_t* out, Select<kT>& sh)
 {
+    constexpr int kCopies = Select<kT>::kCopies;
     constexpr int kWaves = kT / 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     Tokens<kT, kN> x;
@@ -284,8 +304,8 @@ __device__ inline void select_pair(const EvictParams& p, const int32_t* row, int
     // need-th from the top
     const int all = (L + kN * kT - 1) / (kN * kT) * (kN * kT);
     int need = p.keep, candidates = all;
-    auto find_digit = [&](auto in, auto digit) -> unsigned {
-        for (int i = tid; i < kBins; i += kT) sh.bins[i] = 0;
+    auto find_digit = [&](auto in, auto digit, auto of_keys) -> unsigned {
+        for (int i = tid; i < kBins * kCopies; i += kT) sh.bins[0][i] = 0;
         __syncthreads();
         if (candidates < all && candidates > all / 2) {
             // most tokens share the digits so far, so mostly the next one too
@@ -296,15 +316,21 @@ __device__ inline void select_pair(const EvictParams& p, const int32_t* row, int
                 const uint64_t act = __ballot(c);
                 const unsigned d0 = (unsigned)__builtin_amdgcn_readlane((int)d, act ? __builtin_ctzll(act) : 0);
                 if (__ballot(c && d != d0) == 0) {
-                    if (lane == 0 && act) atomicAdd(&sh.bins[d0], (unsigned)__popcll(act));
+                    if (lane == 0 && act) atomicAdd(&sh.bins[d0][0], (unsigned)__popcll(act));
                 } else if (c) {
-                    atomicAdd(&sh.bins[d], 1u);
+                    atomicAdd(&sh.bins[d][lane % kCopies], 1u);
                 }
             }, no_batch);
         } else {
+            // protected tokens share every digit of the key, and often a wave
+            constexpr bool kKeys = decltype(of_keys)::value;
+            int safe = 0;
             walk([&](unsigned key, int t, int) {
-                if (in(key, t)) atomicAdd(&sh.bins[digit(key, t)], 1u);
+                const bool c = in(key, t), top = kKeys && key == 0xffffffffu;
+                if (kKeys) safe += __popcll(__ballot(c && top));
+                if (c && !top) atomicAdd(&sh.bins[digit(key, t)][lane % kCopies], 1u);
             }, no_batch);
+            if (kKeys && lane == 0 && safe > 0) atomicAdd(&sh.bins[digit(0xffffffffu, 0)][0], (unsigned)safe);
         }
         __syncthreads();
         // a thread has kPer bins, counted down from the top: the counts above them
@@ -312,7 +338,12 @@ __device__ inline void select_pair(const EvictParams& p, const int32_t* row, int
         const int top = kBins - 1 - kPer * tid;
         int c[kPer], sum = 0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) sum += c[i] = (int)sh.bins[top - i];
+        for (int i = 0; i < kPer; ++i) {
+            c[i] = 0;
+#pragma unroll
+            for (int j = 0; j < kCopies; ++j) c[i] += (int)sh.bins[top - i][j];
+            sum += c[i];
+        }
         int incl = wave_scan(sum, lane);
         if (lane == 63) sh.wave[wave] = incl;
         __syncthreads();
@@ -345,20 +376,20 @@ __device__ inline void select_pair(const EvictParams& p, const int32_t* row, int
         return key == prefix && (slot_shift == 32 || ~(unsigned)t >> slot_shift == slots);
     };
     if (candidates > kFew) {
-        prefix = find_digit([](unsigned, int) -> bool { return true; }, [](unsigned key, int) -> unsigned { return key >> 21; });
+        prefix = find_digit([](unsigned, int) -> bool { return true; }, [](unsigned key, int) -> unsigned { return key >> 21; }, std::true_type());
         shift = 21;
     }
     while (candidates > kFew && shift > 0) {
         const int to = shift == 21 ? 10 : 0;
         const unsigned dm = to == 0 ? 1023u : 2047u;
-        const unsigned d = find_digit(in_keys, [&](unsigned key, int) -> unsigned { return key >> to & dm; });
+        const unsigned d = find_digit(in_keys, [&](unsigned key, int) -> unsigned { return key >> to & dm; }, std::true_type());
         prefix = prefix << (shift - to) | d;
         shift = to;
     }
     while (candidates > kFew) {   // (slots differ: it ends)
         const int to = slot_shift == 32 ? 21 : slot_shift == 21 ? 10 : 0;
         const unsigned dm = to == 0 ? 1023u : 2047u;
-        const unsigned d = find_digit(in_slots, [&](unsigned, int t) -> unsigned { return ~(unsigned)t >> to & dm; });
+        const unsigned d = find_digit(in_slots, [&](unsigned, int t) -> unsigned { return ~(unsigned)t >> to & dm; }, std::false_type());
         slots = slot_shift == 32 ? d : slots << (slot_shift - to) | d;
         slot_shift = to;
     }
@@ -404,7 +435,7 @@ template <int kT>
 __global__ __launch_bounds__(kT, 4) void select_kernel(EvictParams p)
 {
     __shared__ union {
-        Select select;
+        Select<kT> select;
         Moves<kT> moves;
     } sh;
     const int pair = (int)blockIdx.x, b = pair / p.Hkv, g = pair - b * p.Hkv;

@@ -425,6 +425,43 @@ def test_evict_positions_of_any_size(torch, kv4):
     assert same(got, (cache, w, pos))
 
 
+@pytest.mark.parametrize("keep", [1, 255, 256, 257, 1500, 2047, 4999])
+def test_evict_of_equal_keys(torch, kv4, keep):
+    """All protected alike, all weights alike, and a few among many alike: the
+    slots decide."""
+    for kind in range(3):
+        cache, table, lens, w, pos = evict_case([5000, 300], 1, seed=7)
+        w[...] = 1.5
+        if kind == 0:
+            pos[...] = 0
+        if kind == 2:
+            w[np.random.default_rng(1).random(w.shape) < 0.02] = 2.0
+            w[np.random.default_rng(2).random(w.shape) < 0.02] = -1.0
+        budget = (keep, 1 if kind == 0 else 0, 0)
+        got = run_evict(torch, kv4, cache, table, lens, w, pos, *budget)
+        O.evict(cache, table, lens, w, pos, *budget)
+        assert same(got, (cache, w, pos))
+
+
+@pytest.mark.parametrize("kind", ["normal", "ties"])
+@pytest.mark.parametrize("L,keep,sinks,recent", [(33000, 5000, 4, 1000), (70001, 69000, 0, 0), (40000, 33000, 0, 32768)])
+def test_evict_of_long_pairs(torch, kv4, kind, L, keep, sinks, recent):
+    cache, table, lens, w, pos = evict_case([L], 1, seed=L, kind=kind)
+    got = run_evict(torch, kv4, cache, table, lens, w, pos, keep, sinks, recent)
+    O.evict(cache, table, lens, w, pos, keep, sinks, recent)
+    assert same(got, (cache, w, pos))
+
+
+def test_evict_of_many_pairs(torch, kv4):
+    """More pairs than four for every CU, most of them short of the budget."""
+    lens = np.random.default_rng(3).integers(0, 120, 300)
+    lens[7] = 9000
+    cache, table, lens, w, pos = evict_case(lens, 4, seed=9)
+    got = run_evict(torch, kv4, cache, table, lens, w, pos, 50, 2, 10)
+    O.evict(cache, table, lens, w, pos, 50, 2, 10)
+    assert same(got, (cache, w, pos))
+
+
 def test_evict_leaves_blocks_outside_the_pool_alone(torch, kv4):
     cache, table, lens, w, pos = evict_case([400, 100], 2, seed=5)
     table[0, 3], table[0, 20] = -1, cache.shape[0] + 5
