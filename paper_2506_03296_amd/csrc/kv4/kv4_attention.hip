@@ -301,21 +301,32 @@ struct QueryOperand {
     int scale[G == 8 ? 2 : 1];
 };
 
-template <int G>
-__device__ inline void load_query(const Params& p, int b, int g, int lane, QueryOperand<G>& op)
-{
-    const int col = lane & 15, q = lane >> 4;
-    const int head = G == 8 ? col & 7 : (col & 3) & (G - 1);
-    const f16* row = p.q + ((size_t)b * p.Hq + (size_t)g * G + head) * kHeadDim + 16 * q;
+// A lane's dims of its column's head, as they are.
+struct QueryRow {
     u32x4 w[4];
+};
+
+template <int G>
+__device__ inline void load_row(const Params& p, int b, int g, int lane, QueryRow& q)
+{
+    const int col = lane & 15;
+    const int head = G == 8 ? col & 7 : (col & 3) & (G - 1);
+    const f16* row = p.q + ((size_t)b * p.Hq + (size_t)g * G + head) * kHeadDim + 16 * (lane >> 4);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = *(const u32x4*)(row + (i >> 1) * 64 + (i & 1) * 8);
+    for (int i = 0; i < 4; ++i) q.w[i] = *(const u32x4*)(row + (i >> 1) * 64 + (i & 1) * 8);
+}
+
+template <int G>
+__device__ inline void split_query(unsigned q_sign, const QueryRow& row, int lane, QueryOperand<G>& op)
+{
+    const int col = lane & 15;
+    u32x4 w[4] = {row.w[0], row.w[1], row.w[2], row.w[3]};
     unsigned m = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            w[i][j] ^= p.q_sign * 0x10001u;
+            w[i][j] ^= q_sign * 0x10001u;
             m = max(m, max(w[i][j] & 0x7fffu, (w[i][j] >> 16) & 0x7fffu));
         }
     // as floats the bit patterns of non-negative values order alike; a NaN or
@@ -417,6 +428,8 @@ struct State {
 struct Span {
     const int32_t* bt;    // table entry of the first
     const char* pair;     // slab of kv-head g in block 0
+    uint64_t step;        // bytes from a block to the next
+    unsigned pool;        // blocks
     int first, n;
     int L;
 };
@@ -430,6 +443,8 @@ __device__ inline Span wave_span(const Params& p, int b, int g, int L, int lo, i
     s.n = uniform(max(0, min(hi, s.first + per) - s.first));
     s.bt = p.bt + (size_t)uniform(b) * (size_t)p.stride + (s.n > 0 ? s.first : 0);
     s.pair = apex::uniform_ptr(p.cache + (size_t)uniform(g) * kSlabBytes);
+    s.step = (uint64_t)p.Hkv * kSlabBytes;
+    s.pool = p.num_blocks;
     s.L = uniform(L);
     return s;
 }
@@ -443,6 +458,7 @@ struct Step {
 
 struct Pipe {
     Step x[2];
+    QueryRow q;
 };
 
 __device__ inline unsigned id_at(const Span& s, int i)
@@ -453,21 +469,23 @@ __device__ inline unsigned id_at(const Span& s, int i)
 }
 
 // The slab of a block, with no extent (loads give zeros) outside the pool.
-__device__ inline __amdgpu_buffer_rsrc_t slab_of(const Params& p, const Span& s, unsigned id)
+__device__ inline __amdgpu_buffer_rsrc_t slab_of(const Span& s, unsigned id)
 {
-    return slab_resource(s.pair + id * ((uint64_t)p.Hkv * kSlabBytes), id < p.num_blocks ? kSlabBytes : 0);
+    return slab_resource(s.pair + id * s.step, id < s.pool ? kSlabBytes : 0);
 }
 
-// Asks for a span's first blocks.
-__device__ inline void begin(const Params& p, const Span& s, int lane, Pipe& pipe)
+// Asks for the row of q and a span's first blocks.
+template <int G>
+__device__ inline void begin(const Params& p, int b, int g, const Span& s, int lane, Pipe& pipe)
 {
+    load_row<G>(p, b, g, lane, pipe.q);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         Step& x = pipe.x[i];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             x.id[j] = id_at(s, 2 * i + j);
-            const auto r = slab_of(p, s, x.id[j]);
+            const auto r = slab_of(s, x.id[j]);
             load_keys<0>(x.t[j], r, lane);
             load_values(x.t[j], r, lane);
             x.next[j] = id_at(s, 4 + 2 * i + j);
@@ -477,14 +495,13 @@ __device__ inline void begin(const Params& p, const Span& s, int lane, Pipe& pip
 
 // A wave's attention over its span, whose first blocks are on their way.
 template <int G>
-__device__ inline void attend(const Params& p, int b, int g, const Span& s, int lane, Pipe& pipe, State& st)
+__device__ inline void attend(const Params& p, const Span& s, int lane, Pipe& pipe, State& st)
 {
     const int col = lane & 15, q = lane >> 4;
     const int parity = G == 8 ? col >> 3 : (col >> 2) & 1;
     // bytes 2 and 3 of a weight to the half of its parity, zeros to the other
     const unsigned place = parity ? 0x03020c0cu : 0x0c0c0302u;
     const unsigned low_part = G < 8 && col >= 8 ? 0xffff0000u : 0u;
-    const unsigned pool = p.num_blocks;
     st.m = -INFINITY;
     st.l = 0.f;
 #pragma unroll
@@ -492,11 +509,11 @@ __device__ inline void attend(const Params& p, int b, int g, const Span& s, int 
 
     // q's digits are worked out while the first blocks are on their way
     QueryOperand<G> op;
-    load_query<G>(p, b, g, lane, op);
+    split_query<G>(p.q_sign, pipe.q, lane, op);
 
     // blocks k and k + 1, in x; x is refilled with k + 4 and k + 5
     auto step = [&](Step& x, int k) {
-        const bool good[2] = {x.id[0] < pool, x.id[1] < pool};
+        const bool good[2] = {x.id[0] < s.pool, x.id[1] < s.pool};
         const int tok = (s.first + k) * kBlockSize;
         const bool tail = !good[0] || !good[1] || tok > s.L - 2 * kBlockSize;
         float sc[8];
@@ -515,7 +532,7 @@ __device__ inline void attend(const Params& p, int b, int g, const Span& s, int 
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             x.id[i] = x.next[i];
-            refill[i] = slab_of(p, s, x.id[i]);
+            refill[i] = slab_of(s, x.id[i]);
             load_keys<0>(x.t[i], refill[i], lane);
             x.next[i] = id_at(s, k + 8 + i);
         }
@@ -752,7 +769,7 @@ __device__ inline void store_partial(const Params& p, int64_t slot, int e0, int 
 template <int G>
 __device__ inline void join_partials(const Params& p, int wf, int c0, int c1, int wave, int lane, Shared<G>& sh)
 {
-    constexpr int N = 2 * G, kRows = 8, kVecs = G == 1 ? 1 : N / 4, kPer = N / kVecs;
+    constexpr int N = 2 * G, kRows = G == 8 ? 4 : 8, kVecs = G == 1 ? 1 : N / 4, kPer = N / kVecs;
     typedef typename apex::vec_of<unsigned, kPer>::type word;
     const int h = lane * N / kHeadDim, dim = lane * N % kHeadDim;
     Row<N> r;
@@ -797,10 +814,6 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
     __shared__ Shared<G> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int w = (int)blockIdx.x;
-    // Two waves share a SIMD, which serves the older first: without this the
-    // younger four end 15 % later (one request of 131071 tokens: 22.2 against 19.3
-    // us; with it 20.7 and 21.5)
-    if (wave >= kWaves / 2) __builtin_amdgcn_s_setprio(1);
     Plan plan = make_plan<true>(p, p.Hkv, kPairCost, (unsigned)w, lane);
 
     Pipe pipe;
@@ -818,7 +831,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
             x.g = i - x.b * p.Hkv;
             x.L = uniform(context(p, x.b));
             s = wave_span(p, x.b, x.g, x.L, 0, (int)blocks(x.L), 0, 1);
-            if (s.n > 0) begin(p, s, lane, pipe);
+            if (s.n > 0) begin<G>(p, x.b, x.g, s, lane, pipe);
         };
         Pair x;
         Span s;
@@ -828,7 +841,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
             Row<N> r;
             clear(r);
             State st;
-            if (s.n > 0) attend<G>(p, x.b, x.g, s, lane, pipe, st);
+            if (s.n > 0) attend<G>(p, s, lane, pipe, st);
             const Pair done = x;
             const bool any = s.n > 0;
             i += kWaves * p.workers;
@@ -854,13 +867,13 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
     Span s;
     auto start = [&]() {
         s = wave_span(p, plan.b, plan.g, plan.L, plan.blk, plan.blk + plan.take, wave, kWaves);
-        begin(p, s, lane, pipe);
+        begin<G>(p, plan.b, plan.g, s, lane, pipe);
     };
     if (more) start();
     while (more) {
         const int b = plan.b, g = plan.g, nb = (int)blocks(plan.L);
         State st;
-        attend<G>(p, b, g, s, lane, pipe, st);
+        attend<G>(p, s, lane, pipe, st);
         // the pair's first and last work groups
         int wf = plan.first, wl = plan.last;
         if (plan.way == kLine) {
@@ -935,31 +948,26 @@ template <int G>
 __device__ inline void accumulate(const Params& p, int b, int g, const Span& s, int lane, float* sums)
 {
     const int col = lane & 15, q = lane >> 4;
-    const uint64_t step_bytes = (uint64_t)p.Hkv * kSlabBytes;
-    auto id_at = [&](int i) -> unsigned {
-        const unsigned id = *(const __attribute__((address_space(4))) uint32_t*)(s.bt + (i < s.n ? i : 0));
-        return i < s.n ? id : 0xffffffffu;
-    };
-    auto load = [&](Tile& t, unsigned id) {
-        load_keys<apex::kStreamingLoad>(t, slab_resource(s.pair + id * step_bytes, id < p.num_blocks ? kSlabBytes : 0), lane);
-    };
+    auto load = [&](Tile& t, unsigned id) { load_keys<apex::kStreamingLoad>(t, slab_of(s, id), lane); };
     // the lane's block of a chunk and its four tokens there
     const int own = lane >> 2, tok = 4 * (lane & 3);
     auto own_id = [&](int k) -> unsigned { return k + own < s.n ? (unsigned)s.bt[k + own] : 0xffffffffu; };
     unsigned lane_id = own_id(0);
+    QueryRow row;
+    load_row<G>(p, b, g, lane, row);
     Tile t[kAhead];
     unsigned next[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-        load(t[i], id_at(i));
-        next[i] = id_at(kAhead + i);
+        load(t[i], id_at(s, i));
+        next[i] = id_at(s, kAhead + i);
     }
     QueryOperand<G> op;
-    load_query<G>(p, b, g, lane, op);
+    split_query<G>(p.q_sign, row, lane, op);
     const int head = G == 8 ? col & 7 : (col & 3) & (G - 1);
     const float lse2 = p.lse_in[(size_t)b * p.Hq + (size_t)g * G + head] * 1.4426950408889634f;
     for (int k = 0; k < s.n; k += kChunk) {
-        const bool live = lane_id < p.num_blocks;
+        const bool live = lane_id < s.pool;
         f32x4* const to = (f32x4*)(p.weights + ((uint64_t)(live ? lane_id : 0) * p.Hkv + g) * kBlockSize + tok);
         f32x4 old = {0.f, 0.f, 0.f, 0.f};
         if (live) old = *to;
@@ -973,7 +981,7 @@ __device__ inline void accumulate(const Params& p, int b, int g, const Span& s, 
                 f32x4 w = scores<G>(t[i], op);
                 __builtin_amdgcn_sched_barrier(0);
                 load(t[i], next[i]);
-                next[i] = id_at(k + j + 2 * kAhead + i);
+                next[i] = id_at(s, k + j + 2 * kAhead + i);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     w[e] = apex::exp2_fast(fmaf(w[e], p.scale_log2, -lse2));

@@ -109,14 +109,10 @@ def empty_cache(num_blocks, Hkv, device):
     return torch.empty((num_blocks, Hkv, SLAB_BYTES), dtype=torch.uint8, device=device)
 
 
-def _ready(t, dtype, shape, index):
-    """True if t is a contiguous tensor of this dtype and shape on GPU `index`."""
-    return t.dtype is dtype and t.shape == shape and t.is_cuda and t.get_device() == index and t.is_contiguous()
-
-
-def _want(t, name, dtype, shape, device):
-    """As _ready, with an error for what is not so."""
-    if not _ready(t, dtype, shape, device.index):
+def _want(t, name, dtype, shape, device, index):
+    """An error unless t is a contiguous tensor of this dtype and shape on the
+    device (of that index)."""
+    if not (t.dtype is dtype and t.shape == shape and t.is_cuda and t.get_device() == index and t.is_contiguous()):
         _require(t, name, dtype, device, shape=shape)
 
 
@@ -139,8 +135,8 @@ def _batch(block_table, context_lens, device):
     if block_table.dim() != 2:
         raise ValueError(f"block_table must be [B][entries per row], got {tuple(block_table.shape)}")
     B, stride = block_table.shape
-    _want(block_table, "block_table", i32, (B, stride), device)
-    _want(context_lens, "context_lens", i32, (B,), device)
+    _want(block_table, "block_table", i32, (B, stride), device, device.index)
+    _want(context_lens, "context_lens", i32, (B,), device, device.index)
     return B, stride
 
 
@@ -148,7 +144,7 @@ def _queries(q, B, device):
     """Hq."""
     if q.dim() != 3 or q.shape[0] != B or q.shape[2] != HEAD_DIM:
         raise ValueError(f"q must be [B={B}][Hq][{HEAD_DIM}], got {tuple(q.shape)}")
-    _want(q, "q", _torch().float16, q.shape, device)
+    _want(q, "q", _torch().float16, q.shape, device, device.index)
     return q.shape[1]
 
 
@@ -199,25 +195,29 @@ def append(k_new, v_new, kv_cache, slot_mapping, token_positions=None, positions
     become 0."""
     torch = _torch()
     nb, Hkv, dev, index = _cache(kv_cache)
+    f16 = torch.float16
     if k_new.dim() != 3 or v_new.shape != k_new.shape or k_new.shape[1] != Hkv or k_new.shape[2] != HEAD_DIM:
         raise ValueError(f"k_new and v_new must both be [T][Hkv={Hkv}][{HEAD_DIM}]")
     T = k_new.shape[0]
-    if not (_on(k_new, torch.float16, index) and _on(v_new, torch.float16, index)):
-        _require(k_new, "k_new", torch.float16, dev, contiguous=False)
-        _require(v_new, "v_new", torch.float16, dev, contiguous=False)
+    if not (k_new.dtype is f16 and v_new.dtype is f16 and k_new.is_cuda and v_new.is_cuda
+            and k_new.get_device() == index and v_new.get_device() == index):
+        _require(k_new, "k_new", f16, dev, contiguous=False)
+        _require(v_new, "v_new", f16, dev, contiguous=False)
     ks, vs = k_new.stride(), v_new.stride()
     if ks[2] != 1 or vs[2] != 1 or (Hkv > 1 and (ks[1] != HEAD_DIM or vs[1] != HEAD_DIM)):
         raise ValueError("each token's rows must be contiguous [Hkv][d]")
     if T > 1 and (ks[0] != vs[0] or ks[0] < Hkv * HEAD_DIM):
         raise ValueError("k_new and v_new must share the token stride, at least Hkv * d")
-    _want(slot_mapping, "slot_mapping", torch.int64, (T,), dev)
+    if not (slot_mapping.dtype is torch.int64 and slot_mapping.shape == (T,) and slot_mapping.is_cuda
+            and slot_mapping.get_device() == index and slot_mapping.is_contiguous()):
+        _require(slot_mapping, "slot_mapping", torch.int64, dev, shape=(T,))
     if (positions is None) != (token_positions is None):
         raise ValueError("positions and token_positions go together")
     if positions is not None:
-        _want(token_positions, "token_positions", torch.int32, (T,), dev)
-        _want(positions, "positions", torch.int32, (nb, Hkv, BLOCK_SIZE), dev)
+        _want(token_positions, "token_positions", torch.int32, (T,), dev, index)
+        _want(positions, "positions", torch.int32, (nb, Hkv, BLOCK_SIZE), dev, index)
     if weights is not None:
-        _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev)
+        _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev, index)
     _call("apex_kv4_append", index, k_new.data_ptr(), v_new.data_ptr(), ks[0] if T > 1 else 0, kv_cache.data_ptr(),
           slot_mapping.data_ptr(), None if positions is None else token_positions.data_ptr(),
           None if positions is None else positions.data_ptr(), None if weights is None else weights.data_ptr(),
@@ -231,16 +231,16 @@ def gather(kv_cache, slot_mapping, k_out=None, v_out=None, stream=None):
     torch = _torch()
     nb, Hkv, dev, index = _cache(kv_cache)
     T = slot_mapping.numel()
-    _want(slot_mapping, "slot_mapping", torch.int64, (T,), dev)
+    _want(slot_mapping, "slot_mapping", torch.int64, (T,), dev, index)
     shape = (T, Hkv, HEAD_DIM)
     if k_out is None:
         k_out = torch.empty(shape, dtype=torch.float16, device=dev)
     else:
-        _want(k_out, "k_out", torch.float16, shape, dev)
+        _want(k_out, "k_out", torch.float16, shape, dev, index)
     if v_out is None:
         v_out = torch.empty_like(k_out)
     else:
-        _want(v_out, "v_out", torch.float16, shape, dev)
+        _want(v_out, "v_out", torch.float16, shape, dev, index)
     _call("apex_kv4_gather", index, kv_cache.data_ptr(), slot_mapping.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
           T, Hkv, HEAD_DIM, BLOCK_SIZE, nb, _raw_stream(stream, index))
     return k_out, v_out
@@ -257,9 +257,9 @@ def attention(q, kv_cache, block_table, context_lens, scale, out=None, lse_out=N
     if out is None:
         out = torch.empty_like(q)
     else:
-        _want(out, "out", torch.float16, q.shape, q.device)
+        _want(out, "out", torch.float16, q.shape, q.device, index)
     if lse_out is not None:
-        _want(lse_out, "lse_out", torch.float32, (B, Hq), q.device)
+        _want(lse_out, "lse_out", torch.float32, (B, Hq), q.device, index)
     ws, ws_bytes = (None, 0) if workspace is None else _workspace(workspace, q.device)
     _call("apex_kv4_attention", index, q.data_ptr(), kv_cache.data_ptr(), block_table.data_ptr(), stride,
           context_lens.data_ptr(), out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), B, Hq, Hkv,
@@ -273,8 +273,8 @@ def accumulate_weights(q, kv_cache, block_table, context_lens, scale, lse, weigh
     torch = _torch()
     B, Hq, nb, Hkv, stride, index = _step(q, kv_cache, block_table, context_lens)
     dev = q.device
-    _want(lse, "lse", torch.float32, (B, Hq), dev)
-    _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev)
+    _want(lse, "lse", torch.float32, (B, Hq), dev, index)
+    _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev, index)
     _call("apex_kv4_accumulate_weights", index, q.data_ptr(), kv_cache.data_ptr(), block_table.data_ptr(), stride,
           context_lens.data_ptr(), lse.data_ptr(), weights.data_ptr(), B, Hq, Hkv, HEAD_DIM, BLOCK_SIZE, nb, scale,
           _raw_stream(stream, index))
@@ -295,8 +295,8 @@ def evict(kv_cache, block_table, context_lens, weights, positions, keep, sinks=0
                          "sinks + recent at most keep")
     nb, Hkv, dev, index = _cache(kv_cache)
     B, stride = _batch(block_table, context_lens, dev)
-    _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev)
-    _want(positions, "positions", torch.int32, (nb, Hkv, BLOCK_SIZE), dev)
+    _want(weights, "weights", torch.float32, (nb, Hkv, BLOCK_SIZE), dev, index)
+    _want(positions, "positions", torch.int32, (nb, Hkv, BLOCK_SIZE), dev, index)
     ws, ws_bytes = (None, 0) if workspace is None else _workspace(workspace, dev)
     _call("apex_kv4_evict", index, kv_cache.data_ptr(), block_table.data_ptr(), stride, context_lens.data_ptr(),
           weights.data_ptr(), positions.data_ptr(), B, Hkv, HEAD_DIM, BLOCK_SIZE, nb, keep, sinks, recent, ws, ws_bytes,
