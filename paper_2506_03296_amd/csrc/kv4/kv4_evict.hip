@@ -5,9 +5,10 @@
 // inverted, so no two are equal.  One work group per (request, kv-head) pair
 // finds the keep-th of them: counts of the top digit's values among the
 // candidates, the digit that holds it, the next digit among those, until few
-// candidates are left, which are ranked against each other.  A thread keeps its
-// keys in registers up to kResident tokens a pair, so weights and positions are
-// read once; longer pairs read them again for every digit.
+// candidates are left, which are ranked against each other.  A thread keeps up to
+// 32 keys in registers, so weights and positions are read once; longer pairs read
+// them again for every digit, or, where pairs are few, are spread over work
+// groups, with a launch for every step.
 //
 // What is kept goes into a mask, one bit per slot, and the moves are read off
 // the masks only (they overwrite weights and positions): the i-th evicted slot
@@ -27,7 +28,15 @@ constexpr int kFew = 256;                  // candidates that are ranked directl
 constexpr int kMostPerThread = 32;         // keys that a thread keeps
 constexpr int kAgainPerThread = 16;        // and reads at a time where it keeps none
 constexpr int kSmall = 256, kLarge = 1024; // threads of a work group
+constexpr int kResident = kMostPerThread * kLarge;
 constexpr int kOwnMoves = 1024;
+
+// What is known of the keep-th key: its leading digits, and that it is the
+// need-th from the top of those that have them.
+struct Found {
+    unsigned prefix;
+    int need;
+};
 
 struct EvictParams {
     char* cache;
@@ -40,7 +49,11 @@ struct EvictParams {
     unsigned num_blocks;
     int Hkv, stride, words;
     int keep, sinks, recent;
-    int own_moves;         // select_kernel moves up to so many tokens of a pair itself
+    // of pairs that are spread over work groups
+    int chunks;            // of the longest possible pair
+    int32_t* newest;       // [B][Hkv][chunks] highest position
+    Found* found;          // [B][Hkv][2] after the first and the second digit
+    uint16_t* bins;        // [2][B][Hkv][chunks][kBins]: of digits 1 and 3, of digit 2
 };
 
 __device__ inline int context(const EvictParams& p, int b)
@@ -204,6 +217,42 @@ __global__ __launch_bounds__(kSmall) void move_kernel(EvictParams p)
 
 // --- selection --------------------------------------------------------------------
 
+// The digit that holds the need-th from the top.
+template <int kT>
+struct Digit {
+    int wave[kT / 64];
+    unsigned digit;
+    int above, count;   // with higher digits, with this one
+};
+
+// A thread has kPer bins, counted down from the top: c[0] that of digit kBins - 1
+// - kPer tid.
+template <int kT, int kPer>
+__device__ inline void find_need(const int (&c)[kPer], int need, Digit<kT>& sh)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) sum += c[i];
+    int incl = wave_scan(sum, lane);
+    if (lane == 63) sh.wave[wave] = incl;
+    __syncthreads();
+    for (int i = 0; i < wave; ++i) incl += sh.wave[i];
+    int above = incl - sum;
+    if (above < need && need <= incl) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if (above < need && need <= above + c[i]) {
+                sh.digit = (unsigned)(kBins - 1 - kPer * tid - i);
+                sh.above = above;
+                sh.count = c[i];
+            }
+            above += c[i];
+        }
+    }
+    __syncthreads();
+}
+
 template <int kT>
 struct Select {
     // counts of a digit, in copies by the lane's number: weights have few leading
@@ -213,9 +262,8 @@ struct Select {
     static constexpr int kCopies = kT == kLarge ? 2 : 1;
     unsigned bins[kBins][kCopies];
     uint64_t few[kFew];
-    int wave[kT / 64];
-    unsigned digit;
-    int above, count, few_n;
+    Digit<kT> found;
+    int few_n;
     uint64_t last;
 };
 
@@ -280,9 +328,9 @@ __device__ inline void select_pair(const EvictParams& p, const int32_t* row, int
     }
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) newest = max(newest, __shfl_xor(newest, m, 64));
-    if (lane == 0) sh.wave[wave] = newest;
+    if (lane == 0) sh.found.wave[wave] = newest;
     __syncthreads();
-    for (int i = 0; i < kWaves; ++i) newest = max(newest, sh.wave[i]);
+    for (int i = 0; i < kWaves; ++i) newest = max(newest, sh.found.wave[i]);
     const int64_t recent_from = (int64_t)newest - p.recent;
     if (!kAgain) x.keys(p.sinks, recent_from);
     // f(key, t, i) for every token, the i-th of its thread's batch, then g(first)
@@ -333,37 +381,18 @@ __device__ inline void select_pair(const EvictParams& p, const int32_t* row, int
             if (kKeys && lane == 0 && safe > 0) atomicAdd(&sh.bins[digit(0xffffffffu, 0)][0], (unsigned)safe);
         }
         __syncthreads();
-        // a thread has kPer bins, counted down from the top: the counts above them
         constexpr int kPer = kBins / kT;
-        const int top = kBins - 1 - kPer * tid;
-        int c[kPer], sum = 0;
+        int c[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             c[i] = 0;
 #pragma unroll
-            for (int j = 0; j < kCopies; ++j) c[i] += (int)sh.bins[top - i][j];
-            sum += c[i];
+            for (int j = 0; j < kCopies; ++j) c[i] += (int)sh.bins[kBins - 1 - kPer * tid - i][j];
         }
-        int incl = wave_scan(sum, lane);
-        if (lane == 63) sh.wave[wave] = incl;
-        __syncthreads();
-        for (int i = 0; i < wave; ++i) incl += sh.wave[i];
-        int above = incl - sum;
-        if (above < need && need <= incl) {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                if (above < need && need <= above + c[i]) {
-                    sh.digit = (unsigned)(top - i);
-                    sh.above = above;
-                    sh.count = c[i];
-                }
-                above += c[i];
-            }
-        }
-        __syncthreads();
-        need -= sh.above;
-        candidates = sh.count;
-        return sh.digit;
+        find_need<kT, kPer>(c, need, sh.found);
+        need -= sh.found.above;
+        candidates = sh.found.count;
+        return sh.found.digit;
     };
 
     // the keep-th key from the top, digit by digit: candidates have key >> shift
@@ -427,11 +456,12 @@ __device__ inline void select_pair(const EvictParams& p, const int32_t* row, int
         }
     });
     moved = wave_scan(moved, lane);
-    if (lane == 63) sh.wave[wave] = moved;
+    if (lane == 63) sh.found.wave[wave] = moved;
     __syncthreads();
 }
 
-template <int kT>
+// kLong: pairs of more than kResident tokens are left to spread_kernel.
+template <int kT, bool kLong>
 __global__ __launch_bounds__(kT, 4) void select_kernel(EvictParams p)
 {
     __shared__ union {
@@ -444,6 +474,7 @@ __global__ __launch_bounds__(kT, 4) void select_kernel(EvictParams p)
         if (threadIdx.x == 0) p.counts[pair] = 0;
         return;
     }
+    if (kLong && L > kResident) return;
     const int32_t* row = p.bt + (int64_t)b * p.stride;
     uint64_t* out = p.masks + (int64_t)pair * p.words;
     if (L <= 2 * kT)
@@ -454,11 +485,11 @@ __global__ __launch_bounds__(kT, 4) void select_kernel(EvictParams p)
         select_pair<kT, 16, false>(p, row, g, L, out, sh.select);
     else if (L <= kMostPerThread * kT)
         select_pair<kT, kMostPerThread, false>(p, row, g, L, out, sh.select);
-    else
+    else if (!kLong)
         select_pair<kT, kAgainPerThread, true>(p, row, g, L, out, sh.select);
     int n = 0;
-    for (int i = 0; i < kT / 64; ++i) n += sh.select.wave[i];
-    const bool own = n <= p.own_moves;
+    for (int i = 0; i < kT / 64; ++i) n += sh.select.found.wave[i];
+    const bool own = n <= kOwnMoves;
     if (threadIdx.x == 0) p.counts[pair] = own ? 0 : n;
     if (!own) return;
     // (the masks are this work group's own: the barrier makes them visible)
@@ -468,13 +499,162 @@ __global__ __launch_bounds__(kT, 4) void select_kernel(EvictParams p)
     }
 }
 
+// --- selection over several work groups ---------------------------------------------
+
+constexpr int kChunkKeys = 8;                        // a thread
+constexpr int kChunk = kChunkKeys * kLarge;          // tokens a work group
+
+// A pair's tokens in chunks, a work group each, and a launch for every step that
+// needs all of them: the newest position (step 0), the counts of the three digits
+// of the keys (1 to 3; a chunk's counts fit 16 bits, each work group adds up the
+// chunks' and finds the digit itself), the masks (4).  Of the tokens with the last
+// key the first by slot are kept: the chunks' counts of that digit tell how many
+// come before.
+template <int kStep>
+__global__ __launch_bounds__(kLarge, 4) void spread_kernel(EvictParams p)
+{
+    constexpr int kWaves = kLarge / 64;
+    __shared__ unsigned s_bins[kStep >= 1 && kStep <= 3 ? kBins : 1];
+    __shared__ Digit<kLarge> s_found;
+    __shared__ int s_equal[kChunkKeys * kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int pair = (int)blockIdx.x, chunk = (int)blockIdx.y, b = pair / p.Hkv, g = pair - b * p.Hkv;
+    const int L = context(p, b);
+    if (L <= kResident || L <= p.keep || (int64_t)chunk * kChunk >= L) return;
+    if (kStep == 0 && chunk == 0 && tid == 0) p.counts[pair] = 0;
+    const int chunks = (L - 1) / kChunk + 1, first = chunk * kChunk;
+    int32_t* const newest = p.newest + (int64_t)pair * p.chunks;
+    Tokens<kLarge, kChunkKeys> x;
+    x.load(p, p.bt + (int64_t)b * p.stride, g, L, first);
+    if (kStep == 0) {
+        int high = x.newest();
+#pragma unroll
+        for (int m = 32; m >= 1; m >>= 1) high = max(high, __shfl_xor(high, m, 64));
+        if (lane == 0) s_found.wave[wave] = high;
+        __syncthreads();
+        for (int i = 0; i < kWaves; ++i) high = max(high, s_found.wave[i]);
+        if (tid == 0) newest[chunk] = high;
+        return;
+    }
+
+    // the digit that the launch before counted (asked for before the tokens are
+    // waited for, as the newest position is)
+    Found f = {0, p.keep};
+    const int64_t all_bins = (int64_t)gridDim.x * p.chunks * kBins;
+    uint16_t* const bins = p.bins + (int64_t)pair * p.chunks * kBins;
+    const uint16_t* const counted = bins + (kStep == 3 ? all_bins : 0);
+    int c[2] = {0, 0};
+    if (kStep >= 2) {
+        if (kStep >= 3) f = p.found[(int64_t)pair * 2 + kStep - 3];
+#pragma unroll 8
+        for (int i = 0; i < chunks; ++i) {
+            const unsigned two = ((const unsigned*)(counted + (int64_t)i * kBins))[kBins / 2 - 1 - tid];
+            c[0] += (int)(two >> 16);
+            c[1] += (int)(two & 0xffff);
+        }
+    }
+    int high = INT_MIN;
+    for (int i = lane; i < chunks; i += 64) high = max(high, newest[i]);
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) high = max(high, __shfl_xor(high, m, 64));
+    int before = 0;
+    if (kStep >= 2) {
+        find_need<kLarge, 2>(c, f.need, s_found);
+        f.need -= s_found.above;
+        f.prefix = f.prefix << (kStep == 4 ? 10 : 11) | s_found.digit;
+        if (kStep < 4 && chunk == 0 && tid == 0) p.found[(int64_t)pair * 2 + kStep - 2] = f;
+        if (kStep == 4) {
+            for (int i = lane; i < chunk; i += 64) before += counted[(int64_t)i * kBins + s_found.digit];
+#pragma unroll
+            for (int m = 32; m >= 1; m >>= 1) before += __shfl_xor(before, m, 64);
+        }
+    }
+    x.keys(p.sinks, (int64_t)high - p.recent);
+
+    if (kStep <= 3) {
+        constexpr int kAbove = kStep == 1 ? 32 : kStep == 2 ? 21 : 10, kTo = kStep == 1 ? 21 : kStep == 2 ? 10 : 0;
+        for (int i = tid; i < kBins; i += kLarge) s_bins[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kChunkKeys; ++i) {
+            const bool in = kStep == 1 || x.w[i] >> (kAbove & 31) == f.prefix;
+            const unsigned d = x.w[i] >> kTo & ((1u << (kAbove - kTo)) - 1);
+            // the lanes of the first one's digit count once: protected tokens and
+            // equal weights share theirs
+            const uint64_t act = __ballot(in);
+            const unsigned d0 = (unsigned)__builtin_amdgcn_readlane((int)d, act ? __builtin_ctzll(act) : 0);
+            const int same = __popcll(__ballot(in && d == d0));
+            if (lane == 0 && same > 0) atomicAdd(&s_bins[d0], (unsigned)same);
+            if (in && d != d0) atomicAdd(&s_bins[d], 1u);
+        }
+        __syncthreads();
+        uint16_t* const to = bins + (kStep == 2 ? all_bins : 0) + (int64_t)chunk * kBins;
+        ((unsigned*)to)[tid] = s_bins[2 * tid] | s_bins[2 * tid + 1] << 16;
+        return;
+    }
+
+    // words in the order of their slots: kWaves of every i
+    uint64_t equal[kChunkKeys];
+#pragma unroll
+    for (int i = 0; i < kChunkKeys; ++i) {
+        equal[i] = __ballot(x.w[i] == f.prefix);
+        if (lane == 0) s_equal[i * kWaves + wave] = __popcll(equal[i]);
+    }
+    __syncthreads();
+    static_assert(kChunkKeys * kWaves == 128, "two words a lane");
+    const int e0 = s_equal[2 * lane], e1 = s_equal[2 * lane + 1];
+    int base = before + wave_scan(e0 + e1, lane) - e0 - e1;
+    if (wave & 1) base += e0;
+    uint64_t own = 0;
+#pragma unroll
+    for (int i = 0; i < kChunkKeys; ++i) {
+        const int rank = __shfl(base, (i * kWaves + wave) / 2, 64) + __popcll(equal[i] & ((1ull << lane) - 1));
+        const uint64_t bits = __ballot(x.w[i] > f.prefix || (x.w[i] == f.prefix && rank < f.need));
+        own = lane == i ? bits : own;
+    }
+    const int64_t t = (int64_t)first + lane * kLarge + wave * 64;
+    int moved = 0;
+    if (lane < kChunkKeys && t < L) {
+        p.masks[(int64_t)pair * p.words + (t >> 6)] = own;
+        const int64_t skip = p.keep - t;
+        moved = __popcll(own & (skip <= 0 ? ~0ull : skip >= 64 ? 0ull : ~0ull << skip));
+    }
+    moved = wave_scan(moved, lane);
+    if (lane == 63 && moved > 0) atomicAdd(&p.counts[pair], moved);
+}
+
 int64_t mask_words(int64_t stride) { return (stride * kBlockSize + 63) / 64; }
 
 size_t count_bytes(int B, int Hkv) { return align_up((size_t)B * Hkv * 4, 256); }
 
+size_t mask_bytes(int B, int Hkv, int64_t stride) { return align_up((size_t)B * Hkv * mask_words(stride) * 8, 256); }
+
+// Few pairs, of which some may be longer than a work group's registers, are spread.
+// Measured, a work group a pair against a launch a step, pairs x tokens: 8 x 131072
+// 242 against 88 us, 32 x 131072 366 against 240, 64 x 65536 247 against 221, 96 x
+// 65536 315 against 311, 128 x 65536 380 against 402.  Where all are short after all
+// the idle launches cost 1.5 us each: 8 x 4000 19 against 28 us.
+constexpr int64_t kMostSpread = 64;
+bool spread(int64_t pairs, int64_t stride) { return stride * kBlockSize > kResident && pairs <= kMostSpread; }
+
+int64_t chunks_of(int64_t stride) { return (stride * kBlockSize + kChunk - 1) / kChunk; }
+
 size_t need_bytes(int B, int Hkv, int64_t stride)
 {
-    return count_bytes(B, Hkv) + align_up((size_t)B * Hkv * mask_words(stride) * 8, 256);
+    const size_t pairs = (size_t)B * Hkv, chunks = (size_t)chunks_of(stride);
+    const size_t base = count_bytes(B, Hkv) + mask_bytes(B, Hkv, stride);
+    if (!spread((int64_t)pairs, stride)) return base;
+    return base + align_up(pairs * chunks * 4, 256) + align_up(pairs * 2 * sizeof(Found), 256) + 2 * pairs * chunks * kBins * 2;
+}
+
+// Slots and steps over them stay below 2^31, chunks and pairs within a grid.
+int check_evict(int B, int Hkv, int d, int block_size, int64_t num_blocks, int64_t stride)
+{
+    const int rc = check_batch(B, Hkv, Hkv, d, block_size, num_blocks, stride);
+    if (rc != APEX_OK) return rc;
+    if (stride >= 1 << 24) return fail(APEX_ERR_UNSUPPORTED, "block_table_stride %lld reaches 2^24", (long long)stride);
+    if ((int64_t)B * Hkv >= 1 << 22) return fail(APEX_ERR_UNSUPPORTED, "B * Hkv = %lld reaches 2^22", (long long)B * Hkv);
+    return APEX_OK;
 }
 
 }  // namespace
@@ -482,7 +662,7 @@ size_t need_bytes(int B, int Hkv, int64_t stride)
 extern "C" size_t apex_kv4_evict_workspace_bytes(int B, int Hkv, int64_t block_table_stride)
 {
     apex::clear_error();
-    if (check_batch(B, Hkv, Hkv, kHeadDim, kBlockSize, 0, block_table_stride) != APEX_OK) return 0;
+    if (check_evict(B, Hkv, kHeadDim, kBlockSize, 0, block_table_stride) != APEX_OK) return 0;
     return need_bytes(B, Hkv, block_table_stride);
 }
 
@@ -492,12 +672,11 @@ extern "C" int apex_kv4_evict(void* kv_cache, const int32_t* block_table, int64_
                               size_t workspace_bytes, void* stream)
 {
     apex::clear_error();
-    int rc = check_batch(B, Hkv, Hkv, d, block_size, num_blocks, block_table_stride);
+    int rc = check_evict(B, Hkv, d, block_size, num_blocks, block_table_stride);
     if (rc != APEX_OK) return rc;
     if (keep <= 0 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > keep)
         return fail(APEX_ERR_INVALID_ARG, "keep = %d, sinks = %d, recent = %d: keep must be positive, sinks + recent at most keep",
                     keep, sinks, recent);
-    if ((int64_t)B * Hkv >= 1 << 22) return fail(APEX_ERR_UNSUPPORTED, "B * Hkv = %lld reaches 2^22", (long long)B * Hkv);
     // no request can be longer than keep, no token is in the pool
     const int64_t longest = block_table_stride * kBlockSize;
     if (B == 0 || longest <= keep || num_blocks == 0) return APEX_OK;
@@ -523,7 +702,7 @@ extern "C" int apex_kv4_evict(void* kv_cache, const int32_t* block_table, int64_
     int cus = 0;
     rc = compute_units(&cus);
     if (rc != APEX_OK) return rc;
-    EvictParams p;
+    EvictParams p = EvictParams();
     p.cache = (char*)kv_cache;
     p.bt = block_table;
     p.lens = context_lens;
@@ -543,12 +722,27 @@ extern "C" int apex_kv4_evict(void* kv_cache, const int32_t* block_table, int64_
     // are moved by the work group that selects them; a second launch spreads what
     // is left.
     const int64_t most = longest - keep < keep ? longest - keep : keep;
-    p.own_moves = kOwnMoves;
+    const bool wide = spread(pairs, block_table_stride);
     if (longest <= kMostPerThread * kSmall || pairs >= 4 * cus)
-        select_kernel<kSmall><<<(unsigned)pairs, kSmall, 0, (hipStream_t)stream>>>(p);
-    else
-        select_kernel<kLarge><<<(unsigned)pairs, kLarge, 0, (hipStream_t)stream>>>(p);
-    if ((rc = launched("kv4 evict")) != APEX_OK || most <= kOwnMoves) return rc;
+        select_kernel<kSmall, false><<<(unsigned)pairs, kSmall, 0, (hipStream_t)stream>>>(p);
+    else if (!wide)
+        select_kernel<kLarge, false><<<(unsigned)pairs, kLarge, 0, (hipStream_t)stream>>>(p);
+    else {
+        select_kernel<kLarge, true><<<(unsigned)pairs, kLarge, 0, (hipStream_t)stream>>>(p);
+        p.chunks = (int)chunks_of(block_table_stride);
+        char* at = (char*)p.masks + mask_bytes(B, Hkv, block_table_stride);
+        p.newest = (int32_t*)at;
+        at += align_up((size_t)pairs * p.chunks * 4, 256);
+        p.found = (Found*)at;
+        p.bins = (uint16_t*)(at + align_up((size_t)pairs * 2 * sizeof(Found), 256));
+        const dim3 grid((unsigned)pairs, (unsigned)p.chunks);
+        spread_kernel<0><<<grid, kLarge, 0, (hipStream_t)stream>>>(p);
+        spread_kernel<1><<<grid, kLarge, 0, (hipStream_t)stream>>>(p);
+        spread_kernel<2><<<grid, kLarge, 0, (hipStream_t)stream>>>(p);
+        spread_kernel<3><<<grid, kLarge, 0, (hipStream_t)stream>>>(p);
+        spread_kernel<4><<<grid, kLarge, 0, (hipStream_t)stream>>>(p);
+    }
+    if ((rc = launched("kv4 evict")) != APEX_OK || (!wide && most <= kOwnMoves)) return rc;
     int64_t groups = (most + kSmall - 1) / kSmall;
     if (groups * pairs > 4096) groups = 4096 / pairs > 0 ? 4096 / pairs : 1;
     move_kernel<<<dim3((unsigned)pairs, (unsigned)groups), kSmall, 0, (hipStream_t)stream>>>(p);

@@ -452,6 +452,45 @@ def test_evict_of_long_pairs(torch, kv4, kind, L, keep, sinks, recent):
     assert same(got, (cache, w, pos))
 
 
+@pytest.mark.parametrize("keep,sinks,recent", [(1, 1, 0), (8192, 0, 0), (20000, 4, 9000), (33000, 0, 32000)])
+@pytest.mark.parametrize("kind", ["normal", "ties"])
+def test_evict_of_long_and_short_pairs_together(torch, kv4, kind, keep, sinks, recent):
+    """Lengths on both sides of what a work group's registers hold, of its chunks
+    and of the budget."""
+    lens = [40961, 100, 32769, 32768, 0, 8193]
+    cache, table, lens, w, pos = evict_case(lens, 2, seed=keep, kind=kind)
+    got = run_evict(torch, kv4, cache, table, lens, w, pos, keep, sinks, recent)
+    O.evict(cache, table, lens, w, pos, keep, sinks, recent)
+    assert same(got, (cache, w, pos))
+
+
+@pytest.mark.parametrize("keep", [1, 8191, 8192, 16500])
+def test_evict_of_equal_keys_in_a_long_pair(torch, kv4, keep):
+    """The slots decide, in any chunk."""
+    for kind in range(3):
+        cache, table, lens, w, pos = evict_case([40960], 1, seed=11)
+        w[...] = 0.0
+        if kind == 0:
+            pos[...] = 0
+        if kind == 2:
+            w[np.random.default_rng(1).random(w.shape) < 0.02] = 2.0
+            w[np.random.default_rng(2).random(w.shape) < 0.02] = -1.0
+        budget = (keep, 1 if kind == 0 else 0, 0)
+        got = run_evict(torch, kv4, cache, table, lens, w, pos, *budget)
+        O.evict(cache, table, lens, w, pos, *budget)
+        assert same(got, (cache, w, pos))
+
+
+def test_evict_of_a_long_pair_among_many(torch, kv4):
+    """Too many pairs to spread."""
+    lens = np.random.default_rng(3).integers(0, 120, 70)
+    lens[31] = 33333
+    cache, table, lens, w, pos = evict_case(lens, 1, seed=9)
+    got = run_evict(torch, kv4, cache, table, lens, w, pos, 20000, 4, 3000)
+    O.evict(cache, table, lens, w, pos, 20000, 4, 3000)
+    assert same(got, (cache, w, pos))
+
+
 def test_evict_of_many_pairs(torch, kv4):
     """More pairs than four for every CU, most of them short of the budget."""
     lens = np.random.default_rng(3).integers(0, 120, 300)
@@ -471,6 +510,23 @@ def test_evict_leaves_blocks_outside_the_pool_alone(torch, kv4):
     used = table[0, :25][(table[0, :25] >= 0) & (table[0, :25] < cache.shape[0])]
     others = np.setdiff1d(np.arange(cache.shape[0]), used)
     assert same([x[others] for x in got], [x[others] for x in (cache, w, pos)])
+
+
+def test_evict_of_a_long_pair_leaves_blocks_outside_the_pool_alone(torch, kv4):
+    """Tokens outside the pool weigh less than any in it; with as many in it as the
+    budget keeps, those past the budget go to slots that are not there."""
+    cache, table, lens, w, pos = evict_case([33600, 50], 1, seed=5)
+    keep = 33600 - 3 * BS
+    w[table[0, :3]] = -1.0
+    out = [500, 1000, 2099]
+    table[0, out] = -1, cache.shape[0], 2 ** 31 - 1
+    got = run_evict(torch, kv4, cache, table, lens, w, pos, keep, 0, 0)
+    inside = np.setdiff1d(np.arange(2100), out)
+    used = table[0, inside]
+    others = np.setdiff1d(np.arange(cache.shape[0]), used)
+    assert same([x[others] for x in got], [x[others] for x in (cache, w, pos)])
+    # (the tokens of entries 2097 and 2098 go to entries 500 and 1000)
+    assert same([x[used] for x in got], [x[used] for x in (cache, w, pos)])
 
 
 # --- together ---------------------------------------------------------------------------

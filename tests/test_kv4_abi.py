@@ -115,6 +115,15 @@ def test_refusals(lib, call, kw, rc):
     assert kv4.last_error() != ""
 
 
+def test_an_eviction_of_too_wide_a_table_is_refused(lib):
+    assert evict(lib, B=1, Hkv=1, stride=1 << 24) == UNSUP and "2^24" in kv4.last_error()
+    assert kv4.evict_workspace_bytes(1, 1, 1 << 24) == 0 and kv4.evict_workspace_bytes(1, 1, (1 << 24) - 1) > 0
+    # a token's bit, a pair's count
+    assert kv4.evict_workspace_bytes(65, 1, 2049) == 512 + -(-65 * 513 * 8 // 256) * 256
+    # where pairs may be spread, also two counts of 2048 digits for every chunk
+    assert kv4.evict_workspace_bytes(64, 1, 2049) >= 64 * 5 * 2 * 2048 * 2
+
+
 def test_nothing_to_do(lib):
     assert append(lib, T=0, k=None, v=None, cache=None, slots=None) == A.APEX_OK
     assert gather(lib, T=0, k=None, v=None, cache=None, slots=None) == A.APEX_OK
