@@ -26,6 +26,12 @@
 // value of the cache exactly (fp16 would not hold the largest); the fp32
 // weights go in as two bf16 parts, 16 bits, in columns of their own (G = 8: in
 // two passes), while the normaliser sums them unrounded.
+//
+// Bound by HBM for long batches: 32 requests of 4096-32768 tokens, 8 kv-heads, G =
+// 4, 452 MB in 79 us (5.7 TB/s; plain reads of slabs in the same pattern reach 6.8),
+// one of 131071, 143 MB, in 29.2.  The difference is the launch, the first round trip
+// (table, then slabs), the waves' uneven ends and the joining of split pairs, 6-8 us
+// a call, which is most of a small batch's time (16 of 256-4096, 38 MB, 15.9 us).
 #include <type_traits>
 
 #include "kernels.h"
@@ -938,6 +944,11 @@ __global__ __launch_bounds__(kThreads, 2) void attention_kernel(Params p)
 // the weights with one load and one store of all its lanes (four lanes to a
 // block): a load and a store for every block, by four lanes each, put a store
 // into the wait for every K tile, 37 us against 30 without the stores.
+// Bound by HBM: 24 requests of 2048-16384 tokens, 8 kv-heads, G = 8, 143 MB, take 32.1
+// us (4.5 TB/s, a fifth of it the weights' reads and writes), 16 of 256-4096 at G = 4
+// 9.0.  For the two: 2 work groups a CU 34.1 and 8.7, 4 32.9 and 9.8; 2 tiles on
+// their way 34.3 and 9.2, 8 33.0 and 9.9; a pair cost of 4 32.9 and 10.1, of 64 33.2
+// and 9.6.
 constexpr int kWeightThreads = 256;
 constexpr int kWeightWaves = kWeightThreads / 64;
 constexpr int kWeightGroupsPerCu = 3;

@@ -15,6 +15,12 @@
 // below `keep` takes the i-th kept one from `keep` on.  Sources and targets are
 // disjoint, so the moves need no order, and a cut by a few tokens moves a few
 // rows.
+//
+// 256 pairs of 2048-32768 tokens cut to 4096 take 154 us: 38 to select (8 bytes a
+// token, but three digits' counts, each with its barriers), 100 to move.  A row's
+// values are 4-byte pieces over 256 bytes that it shares with three other tokens,
+// so the moves read 230 MB and write 126 for 190 MB of rows, 3.5 TB/s (a large copy
+// has 4.5).  Short pairs are bound by the launch and some ten round trips.
 #include <type_traits>
 
 #include "kv4_host.h"
@@ -24,11 +30,21 @@ namespace {
 using namespace kv4;
 
 constexpr int kBins = 2048;
-constexpr int kFew = 256;                  // candidates that are ranked directly
+// Candidates that are ranked directly.  Up to 64: the same times; up to 1024: 89 us
+// where it is 60 (32 pairs of 30000 tokens cut to 15000).
+constexpr int kFew = 256;
 constexpr int kMostPerThread = 32;         // keys that a thread keeps
 constexpr int kAgainPerThread = 16;        // and reads at a time where it keeps none
-constexpr int kSmall = 256, kLarge = 1024; // threads of a work group
+// Threads of a work group: the larger where a pair has more tokens than the smaller
+// one's registers hold, but not with pairs for every CU several times over, whose
+// work groups run beside each other.  256 against 1024 threads: 1024 pairs of 1056
+// tokens 23 against 44 us, 2048 of 600 57 against 99; 64 of 13000 84 against 44.
+constexpr int kSmall = 256, kLarge = 1024;
 constexpr int kResident = kMostPerThread * kLarge;
+// Up to so many tokens of a pair are moved by the work group that selects them; more
+// are spread by a second launch.  128 pairs of 1025-1088 tokens cut to 1024 take 16.9
+// us, 18.7 if all go to the second launch; 32 of 4000 cut to 2000 26.6, 61 if none
+// do.
 constexpr int kOwnMoves = 1024;
 
 // What is known of the keep-th key: its leading digits, and that it is the
@@ -718,9 +734,7 @@ extern "C" int apex_kv4_evict(void* kv_cache, const int32_t* block_table, int64_
     p.sinks = sinks;
     p.recent = recent;
     const int pairs = B * Hkv;
-    // at most min(keep, longest - keep) tokens of a pair move.  Up to kOwnMoves
-    // are moved by the work group that selects them; a second launch spreads what
-    // is left.
+    // at most min(keep, longest - keep) tokens of a pair move
     const int64_t most = longest - keep < keep ? longest - keep : keep;
     const bool wide = spread(pairs, block_table_stride);
     if (longest <= kMostPerThread * kSmall || pairs >= 4 * cus)

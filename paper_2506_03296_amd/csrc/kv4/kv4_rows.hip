@@ -6,7 +6,7 @@
 // a work group sixteen: where they lie in consecutive slots, as a prompt's do,
 // a wave's codes are 256 contiguous bytes of K and of V, and the work group
 // writes (or reads) whole slabs.  Bound by HBM for prompts (5.4 TB/s of reads
-// and writes together; a large copy has 4.8), by the launch and two round trips
+// and writes together; a large copy has 4.5-4.8), by the launch and two round trips
 // for a decode step.
 #include "kv4_host.h"
 
