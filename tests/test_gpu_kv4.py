@@ -637,6 +637,32 @@ def test_captured_and_replayed(torch, kv4):
                 assert torch.equal(x, y)
 
 
+def test_an_eviction_of_long_pairs_captured_and_replayed(torch, kv4):
+    """Steps in several launches, over what the workspace holds from before."""
+    cache, table, lens, w, pos = evict_case([33001, 700], 2, seed=31, kind="ties")
+    budget = (20000, 4, 5000)
+    dt, dl = dev(torch, table, lens)
+    first = dev(torch, cache, w, pos)
+    O.evict(cache, table, lens, w, pos, *budget)
+    ws = torch.full((kv4.evict_workspace_bytes(2, 2, table.shape[1]),), 255, dtype=torch.uint8, device="cuda")
+    buf = [x.clone() for x in first]
+    g = torch.cuda.CUDAGraph()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=s):
+        kv4.evict(buf[0], dt, dl, buf[1], buf[2], *budget, workspace=ws)
+    for i in range(4):
+        for x, y in zip(buf, first):
+            x.copy_(y)
+        if i == 2:
+            ws.fill_(255)
+        g.replay()
+        assert same([x.cpu().numpy() for x in buf], (cache, w, pos))
+        own = [x.clone() for x in first]
+        kv4.evict(own[0], dt, dl, own[1], own[2], *budget)
+        assert all(torch.equal(x, y) for x, y in zip(own, buf))
+
+
 def test_capture_without_a_workspace_is_refused(torch, kv4):
     q, cache, table, lens = case([30], 4, 1, seed=1)
     dq, dc, dt, dl = dev(torch, q, cache, table, lens)
