@@ -115,17 +115,20 @@ int apex_kv4_accumulate_weights(const void* q, const void* kv_cache, const int32
                                 int64_t num_blocks, float scale, void* stream);
 
 /*
- * Evicts tokens: of every request with L_b > keep, each kv-head keeps `keep`
- * tokens, in the slots of positions [0, keep) of its table row, and the
+ * Evicts tokens: of every request with more than `keep` tokens, each kv-head
+ * keeps `keep` of them, in the first `keep` slots of its table row, and the
  * request's new length is keep (the caller's to set; its further blocks are
- * free).  Requests with L_b <= keep are left as they are.
+ * free).  Other requests are left as they are.  Only tokens and slots of the pool
+ * count: in a row with ids outside it, the request's new length is up to the
+ * keep-th slot of the pool, the slots outside before that included, and a request
+ * with no more than `keep` tokens in the pool stays as long as it is.
  * Kept are, of each (request, kv-head): first the protected tokens, all alike,
  * those with a position below `sinks` or among the `recent` highest (position >
  * highest - recent), then the heaviest by weights; equal ones in the order of
  * their slots.  A NaN weighs as -infinity.  sinks + recent <= keep.
- * Tokens kept in [0, keep) stay where they are; the i-th evicted slot there
- * takes the i-th kept token from [keep, L_b), both counted upwards: its K and V
- * row, weight and position.  Slots from keep on are left as they are.  (The
+ * Tokens kept in the first `keep` slots stay where they are; the i-th evicted
+ * slot there takes the i-th kept token from behind them, both counted upwards: its
+ * K and V row, weight and position.  The slots behind are left as they are.  (The
  * attention does not depend on the order of the cached tokens; positions keeps
  * track of it.)  A block may occur only once in the call's table rows.
  * workspace: apex_kv4_evict_workspace_bytes bytes, 256-byte aligned, any content,

@@ -128,12 +128,12 @@ def kept_tokens(w, pos, keep, sinks, recent):
 
 
 def evict(cache, table, lens, weights, positions, keep, sinks, recent):
-    """In place on cache, weights and positions."""
-    for b, L in enumerate(int(x) for x in lens):
-        L = min(L, table.shape[1] * BS)
-        if L <= keep:
+    """In place on cache, weights and positions.  Tokens and slots are those of
+    the pool, in the order of the table row."""
+    for b, L in enumerate(lens):
+        t = live_tokens(table[b], L, cache.shape[0])
+        if len(t) <= keep:
             continue
-        t = np.arange(L)
         block, at = table[b][t // BS], t % BS
         for g in range(cache.shape[1]):
             kept = kept_tokens(weights[block, g, at], positions[block, g, at], keep, sinks, recent)

@@ -12,9 +12,14 @@
 //
 // What is kept goes into a mask, one bit per slot, and the moves are read off
 // the masks only (they overwrite weights and positions): the i-th evicted slot
-// below `keep` takes the i-th kept one from `keep` on.  Sources and targets are
-// disjoint, so the moves need no order, and a cut by a few tokens moves a few
+// of the first `keep` takes the i-th kept one behind them.  Sources and targets
+// are disjoint, so the moves need no order, and a cut by a few tokens moves a few
 // rows.
+//
+// Slots of blocks outside the pool are none of these: they have key 0, below every
+// token's, the first `keep` slots end where the next one of the pool lies (at `keep`
+// itself unless ids before it are outside the pool), and up to there such a slot's
+// bit says "kept", so that nothing is moved to it.
 //
 // 256 pairs of 2048-32768 tokens cut to 4096 take 154 us: 38 to select (8 bytes a
 // token, but three digits' counts, each with its barriers), 100 to move.  A row's
@@ -23,11 +28,13 @@
 // has 4.5).  Short pairs are bound by the launch and some ten round trips.
 #include <type_traits>
 
+#include "kernels.h"
 #include "kv4_host.h"
 
 namespace {
 
 using namespace kv4;
+using apex::uniform;
 
 constexpr int kBins = 2048;
 // Candidates that are ranked directly.  Up to 64: the same times; up to 1024: 89 us
@@ -46,6 +53,7 @@ constexpr int kResident = kMostPerThread * kLarge;
 // us, 18.7 if all go to the second launch; 32 of 4000 cut to 2000 26.6, 61 if none
 // do.
 constexpr int kOwnMoves = 1024;
+constexpr int kGaps = INT_MIN;             // beside a count of moves
 
 // What is known of the keep-th key: its leading digits, and that it is the
 // need-th from the top of those that have them.
@@ -61,13 +69,13 @@ struct EvictParams {
     float* weights;
     int32_t* positions;
     uint64_t* masks;       // [B][Hkv][words], bit i of word w: slot 64 w + i is kept
-    int32_t* counts;       // [B][Hkv] tokens left to move
+    int32_t* counts;       // [B][Hkv] tokens left to move; kGaps: its `keep` slots do not end at `keep`
     unsigned num_blocks;
     int Hkv, stride, words;
     int keep, sinks, recent;
     // of pairs that are spread over work groups
     int chunks;            // of the longest possible pair
-    int32_t* newest;       // [B][Hkv][chunks] highest position
+    int2* newest;          // [B][Hkv][chunks] highest position, tokens in the pool
     Found* found;          // [B][Hkv][2] after the first and the second digit
     uint16_t* bins;        // [2][B][Hkv][chunks][kBins]: of digits 1 and 3, of digit 2
 };
@@ -104,6 +112,38 @@ __device__ inline int wave_scan(int x, int lane)
     return x;
 }
 
+// Where the slot of the pool lies that has `before` of its kind ahead of it among
+// slots [first, last) of a row (first a multiple of the block); 0 if there is none.
+template <int kT>
+__device__ inline int pool_slot(const EvictParams& p, const int32_t* row, int first, int last, int before, int (&sums)[kT / 64],
+                                int& found)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int e0 = first / kBlockSize, n = (last - first + kBlockSize - 1) / kBlockSize, per = (n + kT - 1) / kT;
+    const int a = e0 + min(n, tid * per), e = e0 + min(n, (tid + 1) * per);
+    auto slots = [&](int i) -> int { return (unsigned)row[i] < p.num_blocks ? min(kBlockSize, last - i * kBlockSize) : 0; };
+    int sum = 0;
+    for (int i = a; i < e; ++i) sum += slots(i);
+    int incl = wave_scan(sum, lane);
+    if (lane == 63) sums[wave] = incl;
+    if (tid == 0) found = 0;
+    __syncthreads();
+    for (int i = 0; i < wave; ++i) incl += sums[i];
+    int left = before - (incl - sum);
+    if (left >= 0 && left < sum) {
+        int i = a;
+        for (int s = slots(i); left >= s; s = slots(i)) {
+            left -= s;
+            ++i;
+        }
+        found = i * kBlockSize + left;
+    }
+    __syncthreads();
+    const int at = found;
+    __syncthreads();   // (the caller may write both again)
+    return at;
+}
+
 // --- moves ------------------------------------------------------------------------
 
 template <int kN>
@@ -114,24 +154,25 @@ struct Moves {
     int hole_n, mover_n;
 };
 
-// Moves r0 .. r0 + kN of a pair's n, by kN threads.
+// Moves r0 .. r0 + kN of a pair's n, by kN threads; its first `keep` slots end at
+// slot `end`.
 template <int kN>
-__device__ inline void move_rows(const EvictParams& p, const int32_t* row, int g, const uint64_t* kept, int L, int r0, int n,
-                                 Moves<kN>& sh)
+__device__ inline void move_rows(const EvictParams& p, const int32_t* row, int g, const uint64_t* kept, int L, int end, int r0,
+                                 int n, Moves<kN>& sh)
 {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, keep = p.keep;
-    // a thread counts the holes (evicted below keep) and movers (kept from keep
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    // a thread counts the holes (evicted below end) and movers (kept from end
     // on) of consecutive words and a scan ranks them; the words with any of the
     // kN looked for, at most kN, are put down, and a wave lists a word's slots, a
     // lane each
     const int words = (L + 63) / 64, per = (words + kN - 1) / kN;
     const int a = min(words, tid * per), e = min(words, a + per);
     auto hole_bits = [&](int w) -> uint64_t {
-        const int left = keep - w * 64;
+        const int left = end - w * 64;
         return ~kept[w] & (left <= 0 ? 0ull : left >= 64 ? ~0ull : (1ull << left) - 1);
     };
     auto mover_bits = [&](int w) -> uint64_t {
-        const int skip = keep - w * 64;
+        const int skip = end - w * 64;
         return kept[w] & (skip <= 0 ? ~0ull : skip >= 64 ? 0ull : ~0ull << skip);
     };
     int holes = 0, movers = 0;
@@ -224,9 +265,12 @@ __global__ __launch_bounds__(kSmall) void move_kernel(EvictParams p)
 {
     __shared__ Moves<kSmall> sh;
     const int pair = (int)blockIdx.x, b = pair / p.Hkv, g = pair - b * p.Hkv;
-    const int n = p.counts[pair], L = context(p, b);
+    const int32_t* row = p.bt + (int64_t)b * p.stride;
+    const int count = p.counts[pair], n = count & ~kGaps, L = context(p, b);
+    if ((int)blockIdx.y * kSmall >= n) return;
+    const int end = count & kGaps ? pool_slot<kSmall>(p, row, 0, L, p.keep, sh.holes, sh.hole_n) : p.keep;
     for (int r0 = (int)blockIdx.y * kSmall; r0 < n; r0 += (int)gridDim.y * kSmall) {
-        move_rows<kSmall>(p, p.bt + (int64_t)b * p.stride, g, p.masks + (int64_t)pair * p.words, L, r0, n, sh);
+        move_rows<kSmall>(p, row, g, p.masks + (int64_t)pair * p.words, L, end, r0, n, sh);
         __syncthreads();
     }
 }
@@ -279,6 +323,7 @@ struct Select {
     unsigned bins[kBins][kCopies];
     uint64_t few[kFew];
     Digit<kT> found;
+    int2 seen[kT / 64];   // of a wave's tokens: highest position, whether some lie outside the pool
     int few_n;
     uint64_t last;
 };
@@ -320,6 +365,12 @@ struct Tokens {
         for (int i = 0; i < kN; ++i) n = max(n, live >> i & 1 ? pos[i] : INT_MIN);
         return n;
     }
+    // whether some of the thread's tokens lie outside the pool
+    __device__ inline bool gaps(int L, int first) const
+    {
+        const int n = L - first - (int)threadIdx.x;   // (kT tokens on, the thread's next)
+        return __popc(live) < (n <= 0 ? 0 : min(kN, (n + kT - 1) / kT));
+    }
     __device__ inline void keys(int sinks, int64_t recent_from)
     {
 #pragma unroll
@@ -330,23 +381,32 @@ struct Tokens {
     }
 };
 
+// Returns where the first `keep` slots end, 0 if the pair is left as it is.
 template <int kT, int kN, bool kAgain>
-__device__ inline void select_pair(const EvictParams& p, const int32_t* row, int g, int L, uint64_t* out, Select<kT>& sh)
+__device__ inline int select_pair(const EvictParams& p, const int32_t* row, int g, int L, uint64_t* out, Select<kT>& sh)
 {
     constexpr int kCopies = Select<kT>::kCopies;
     constexpr int kWaves = kT / 64;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     Tokens<kT, kN> x;
-    int newest = INT_MIN;
+    int newest = INT_MIN, gaps = 0;
     for (int first = 0; first == 0 || (kAgain && first < L); first += kN * kT) {
         x.load(p, row, g, L, first);
         newest = max(newest, x.newest());
+        gaps |= x.gaps(L, first);
     }
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) newest = max(newest, __shfl_xor(newest, m, 64));
-    if (lane == 0) sh.found.wave[wave] = newest;
+    gaps = __ballot(gaps) != 0;
+    if (lane == 0) sh.seen[wave] = make_int2(newest, gaps);
     __syncthreads();
-    for (int i = 0; i < kWaves; ++i) newest = max(newest, sh.found.wave[i]);
+    for (int i = 0; i < kWaves; ++i) {
+        newest = max(newest, sh.seen[i].x);
+        gaps |= sh.seen[i].y;
+    }
+    gaps = uniform(gaps);
+    const int end = gaps ? pool_slot<kT>(p, row, 0, L, p.keep, sh.found.wave, sh.few_n) : p.keep;
+    if (end == 0) return 0;   // no more than `keep` tokens
     const int64_t recent_from = (int64_t)newest - p.recent;
     if (!kAgain) x.keys(p.sinks, recent_from);
     // f(key, t, i) for every token, the i-th of its thread's batch, then g(first)
@@ -459,7 +519,8 @@ __device__ inline void select_pair(const EvictParams& p, const int32_t* row, int
     int moved = 0;
     unsigned lo = 0, hi = 0;
     walk([&](unsigned key, int t, int i) {
-        const uint64_t bits = __ballot(key > last_key || (key == last_key && t <= last_t));
+        uint64_t bits = __ballot(key > last_key || (key == last_key && t <= last_t));
+        if (gaps) bits |= __ballot(key == 0 && t < end);
         lo = lane == i ? (unsigned)bits : lo;
         hi = lane == i ? (unsigned)(bits >> 32) : hi;
     }, [&](int first) {
@@ -467,13 +528,14 @@ __device__ inline void select_pair(const EvictParams& p, const int32_t* row, int
         if (lane < kN && t < L) {
             const uint64_t bits = (uint64_t)hi << 32 | lo;
             out[t >> 6] = bits;
-            const int skip = p.keep - t;
+            const int skip = end - t;
             moved += __popcll(bits & (skip <= 0 ? ~0ull : skip >= 64 ? 0ull : ~0ull << skip));
         }
     });
     moved = wave_scan(moved, lane);
     if (lane == 63) sh.found.wave[wave] = moved;
     __syncthreads();
+    return end;
 }
 
 // kLong: pairs of more than kResident tokens are left to spread_kernel.
@@ -493,25 +555,27 @@ __global__ __launch_bounds__(kT, 4) void select_kernel(EvictParams p)
     if (kLong && L > kResident) return;
     const int32_t* row = p.bt + (int64_t)b * p.stride;
     uint64_t* out = p.masks + (int64_t)pair * p.words;
+    int end = 0;
     if (L <= 2 * kT)
-        select_pair<kT, 2, false>(p, row, g, L, out, sh.select);
+        end = select_pair<kT, 2, false>(p, row, g, L, out, sh.select);
     else if (L <= 8 * kT)
-        select_pair<kT, 8, false>(p, row, g, L, out, sh.select);
+        end = select_pair<kT, 8, false>(p, row, g, L, out, sh.select);
     else if (L <= 16 * kT)
-        select_pair<kT, 16, false>(p, row, g, L, out, sh.select);
+        end = select_pair<kT, 16, false>(p, row, g, L, out, sh.select);
     else if (L <= kMostPerThread * kT)
-        select_pair<kT, kMostPerThread, false>(p, row, g, L, out, sh.select);
+        end = select_pair<kT, kMostPerThread, false>(p, row, g, L, out, sh.select);
     else if (!kLong)
-        select_pair<kT, kAgainPerThread, true>(p, row, g, L, out, sh.select);
+        end = select_pair<kT, kAgainPerThread, true>(p, row, g, L, out, sh.select);
     int n = 0;
-    for (int i = 0; i < kT / 64; ++i) n += sh.select.found.wave[i];
+    if (end > 0)
+        for (int i = 0; i < kT / 64; ++i) n += sh.select.found.wave[i];
     const bool own = n <= kOwnMoves;
-    if (threadIdx.x == 0) p.counts[pair] = own ? 0 : n;
+    if (threadIdx.x == 0) p.counts[pair] = own ? 0 : end == p.keep ? n : n | kGaps;
     if (!own) return;
     // (the masks are this work group's own: the barrier makes them visible)
     for (int r0 = 0; r0 < n; r0 += kT) {
         __syncthreads();
-        move_rows<kT>(p, row, g, out, L, r0, n, sh.moves);
+        move_rows<kT>(p, row, g, out, L, end, r0, n, sh.moves);
     }
 }
 
@@ -521,7 +585,7 @@ constexpr int kChunkKeys = 8;                        // a thread
 constexpr int kChunk = kChunkKeys * kLarge;          // tokens a work group
 
 // A pair's tokens in chunks, a work group each, and a launch for every step that
-// needs all of them: the newest position (step 0), the counts of the three digits
+// needs all of them: the newest position and the tokens in the pool (step 0), the counts of the three digits
 // of the keys (1 to 3; a chunk's counts fit 16 bits, each work group adds up the
 // chunks' and finds the digit itself), the masks (4).  Of the tokens with the last
 // key the first by slot are kept: the chunks' counts of that digit tell how many
@@ -539,17 +603,27 @@ __global__ __launch_bounds__(kLarge, 4) void spread_kernel(EvictParams p)
     if (L <= kResident || L <= p.keep || (int64_t)chunk * kChunk >= L) return;
     if (kStep == 0 && chunk == 0 && tid == 0) p.counts[pair] = 0;
     const int chunks = (L - 1) / kChunk + 1, first = chunk * kChunk;
-    int32_t* const newest = p.newest + (int64_t)pair * p.chunks;
+    int2* const newest = p.newest + (int64_t)pair * p.chunks;
     Tokens<kLarge, kChunkKeys> x;
     x.load(p, p.bt + (int64_t)b * p.stride, g, L, first);
     if (kStep == 0) {
-        int high = x.newest();
+        int high = x.newest(), live = __popc(x.live);
 #pragma unroll
-        for (int m = 32; m >= 1; m >>= 1) high = max(high, __shfl_xor(high, m, 64));
-        if (lane == 0) s_found.wave[wave] = high;
+        for (int m = 32; m >= 1; m >>= 1) {
+            high = max(high, __shfl_xor(high, m, 64));
+            live += __shfl_xor(live, m, 64);
+        }
+        if (lane == 0) {
+            s_found.wave[wave] = high;
+            s_equal[wave] = live;
+        }
         __syncthreads();
-        for (int i = 0; i < kWaves; ++i) high = max(high, s_found.wave[i]);
-        if (tid == 0) newest[chunk] = high;
+        live = 0;
+        for (int i = 0; i < kWaves; ++i) {
+            high = max(high, s_found.wave[i]);
+            live += s_equal[i];
+        }
+        if (tid == 0) newest[chunk] = make_int2(high, live);
         return;
     }
 
@@ -569,10 +643,18 @@ __global__ __launch_bounds__(kLarge, 4) void spread_kernel(EvictParams p)
             c[1] += (int)(two & 0xffff);
         }
     }
-    int high = INT_MIN;
-    for (int i = lane; i < chunks; i += 64) high = max(high, newest[i]);
+    int high = INT_MIN, live = 0;
+    for (int i = lane; i < chunks; i += 64) {
+        const int2 of = newest[i];
+        high = max(high, of.x);
+        live += of.y;
+    }
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) high = max(high, __shfl_xor(high, m, 64));
+    for (int m = 32; m >= 1; m >>= 1) {
+        high = max(high, __shfl_xor(high, m, 64));
+        live += __shfl_xor(live, m, 64);
+    }
+    if (live <= p.keep) return;   // (the same for all of the pair's work groups)
     int before = 0;
     if (kStep >= 2) {
         find_need<kLarge, 2>(c, f.need, s_found);
@@ -609,6 +691,25 @@ __global__ __launch_bounds__(kLarge, 4) void spread_kernel(EvictParams p)
         return;
     }
 
+    // where the first `keep` slots end: in the chunk that holds the next one of the pool
+    int end = p.keep;
+    if (live < L) {
+        int ahead = 0, at = 0;
+        for (;; at += 64) {   // (it is there: live > keep)
+            const int of = at + lane < chunks ? newest[at + lane].y : 0, incl = wave_scan(of, lane);
+            const uint64_t hit = __ballot(ahead + incl > p.keep);
+            const int ln = hit ? __builtin_ctzll(hit) : 63;
+            ahead += __shfl(hit ? incl - of : incl, ln, 64);
+            if (hit) {
+                at += ln;
+                break;
+            }
+        }
+        end = pool_slot<kLarge>(p, p.bt + (int64_t)b * p.stride, at * kChunk, min(L, (at + 1) * kChunk), p.keep - ahead,
+                                s_found.wave, s_equal[0]);
+        if (chunk == 0 && tid == 0 && end != p.keep) atomicAdd(&p.counts[pair], kGaps);
+    }
+
     // words in the order of their slots: kWaves of every i
     uint64_t equal[kChunkKeys];
 #pragma unroll
@@ -625,14 +726,15 @@ __global__ __launch_bounds__(kLarge, 4) void spread_kernel(EvictParams p)
 #pragma unroll
     for (int i = 0; i < kChunkKeys; ++i) {
         const int rank = __shfl(base, (i * kWaves + wave) / 2, 64) + __popcll(equal[i] & ((1ull << lane) - 1));
-        const uint64_t bits = __ballot(x.w[i] > f.prefix || (x.w[i] == f.prefix && rank < f.need));
+        const uint64_t bits = __ballot(x.w[i] > f.prefix || (x.w[i] == f.prefix && rank < f.need) ||
+                                       (x.w[i] == 0 && first + i * kLarge + tid < end));
         own = lane == i ? bits : own;
     }
     const int64_t t = (int64_t)first + lane * kLarge + wave * 64;
     int moved = 0;
     if (lane < kChunkKeys && t < L) {
         p.masks[(int64_t)pair * p.words + (t >> 6)] = own;
-        const int64_t skip = p.keep - t;
+        const int64_t skip = end - t;
         moved = __popcll(own & (skip <= 0 ? ~0ull : skip >= 64 ? 0ull : ~0ull << skip));
     }
     moved = wave_scan(moved, lane);
@@ -660,7 +762,7 @@ size_t need_bytes(int B, int Hkv, int64_t stride)
     const size_t pairs = (size_t)B * Hkv, chunks = (size_t)chunks_of(stride);
     const size_t base = count_bytes(B, Hkv) + mask_bytes(B, Hkv, stride);
     if (!spread((int64_t)pairs, stride)) return base;
-    return base + align_up(pairs * chunks * 4, 256) + align_up(pairs * 2 * sizeof(Found), 256) + 2 * pairs * chunks * kBins * 2;
+    return base + align_up(pairs * chunks * sizeof(int2), 256) + align_up(pairs * 2 * sizeof(Found), 256) + 2 * pairs * chunks * kBins * 2;
 }
 
 // Slots and steps over them stay below 2^31, chunks and pairs within a grid.
@@ -745,8 +847,8 @@ extern "C" int apex_kv4_evict(void* kv_cache, const int32_t* block_table, int64_
         select_kernel<kLarge, true><<<(unsigned)pairs, kLarge, 0, (hipStream_t)stream>>>(p);
         p.chunks = (int)chunks_of(block_table_stride);
         char* at = (char*)p.masks + mask_bytes(B, Hkv, block_table_stride);
-        p.newest = (int32_t*)at;
-        at += align_up((size_t)pairs * p.chunks * 4, 256);
+        p.newest = (int2*)at;
+        at += align_up((size_t)pairs * p.chunks * sizeof(int2), 256);
         p.found = (Found*)at;
         p.bins = (uint16_t*)(at + align_up((size_t)pairs * 2 * sizeof(Found), 256));
         const dim3 grid((unsigned)pairs, (unsigned)p.chunks);

@@ -284,7 +284,10 @@ def evict(kv_cache, block_table, context_lens, weights, positions, keep, sinks=0
           stream=None):
     """apex_kv4_evict over torch tensors (in place on the cache, ``weights`` and
     ``positions``).  A request longer than ``keep`` has the length ``keep``
-    afterwards; context_lens is left to the caller.
+    afterwards; context_lens is left to the caller.  In a table row with block ids
+    outside the pool only the tokens in the pool count: the first ``keep`` of their
+    slots hold what is kept, and the length goes up to the last of these (a request
+    with no more than ``keep`` tokens in the pool keeps its length).
 
     ``workspace`` is an optional uint8 tensor of evict_workspace_bytes(B, Hkv,
     block_table.shape[1]) bytes; calls that can overlap, and a captured graph,
