@@ -12,7 +12,10 @@ names and semantics follow include/apex_kv4.h.
 
 block_table int32 [B][entries per row], context_lens int32 [B]; weights fp32
 and positions int32, both [num_blocks][Hkv][16], belong to the cached tokens.
-All tensors are on one GPU; a call works on that device's current stream.
+All tensors are on one GPU; a call works on ``stream``, by default that device's
+current stream.  A result that the call allocates belongs to the stream it works
+on: to use it on another one, wait for the call there, and record_stream before it
+is dropped, as with any tensor of torch's.
 """
 import ctypes
 import os
@@ -179,6 +182,16 @@ def _step(q, kv_cache, block_table, context_lens):
     return B, _queries(q, B, dev), nb, Hkv, stride, index
 
 
+def _rows(shape, device, stream):
+    """Memory for a result, of the stream that writes it: the earlier work on it is
+    that stream's too, and it goes back there when it is dropped."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=torch.float16, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=torch.float16, device=device)
+
+
 def _workspace(workspace, device):
     if not (_on(workspace, _torch().uint8, device.index) and workspace.is_contiguous()):
         _require(workspace, "workspace", _torch().uint8, device)
@@ -234,11 +247,11 @@ def gather(kv_cache, slot_mapping, k_out=None, v_out=None, stream=None):
     _want(slot_mapping, "slot_mapping", torch.int64, (T,), dev, index)
     shape = (T, Hkv, HEAD_DIM)
     if k_out is None:
-        k_out = torch.empty(shape, dtype=torch.float16, device=dev)
+        k_out = _rows(shape, dev, stream)
     else:
         _want(k_out, "k_out", torch.float16, shape, dev, index)
     if v_out is None:
-        v_out = torch.empty_like(k_out)
+        v_out = torch.empty_like(k_out) if stream is None else _rows(shape, dev, stream)
     else:
         _want(v_out, "v_out", torch.float16, shape, dev, index)
     _call("apex_kv4_gather", index, kv_cache.data_ptr(), slot_mapping.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
@@ -255,7 +268,7 @@ def attention(q, kv_cache, block_table, context_lens, scale, out=None, lse_out=N
     torch = _torch()
     B, Hq, nb, Hkv, stride, index = _step(q, kv_cache, block_table, context_lens)
     if out is None:
-        out = torch.empty_like(q)
+        out = torch.empty_like(q) if stream is None else _rows(q.shape, q.device, stream)
     else:
         _want(out, "out", torch.float16, q.shape, q.device, index)
     if lse_out is not None:
