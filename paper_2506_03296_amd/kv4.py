@@ -20,7 +20,7 @@ is dropped, as with any tensor of torch's.
 import ctypes
 import os
 
-from . import APEX_ERR_HIP, APEX_OK, ApexError, _on, _raw_stream, _require, _torch
+from . import APEX_ERR_HIP, APEX_OK, ApexError, _on, _raw_stream, _require, _result, _torch
 
 __all__ = ["LIB_PATH", "EXPORTED_SYMBOLS", "SLAB_BYTES", "BLOCK_SIZE", "HEAD_DIM", "load_library", "last_error",
            "empty_cache", "append", "gather", "attention", "accumulate_weights", "evict",
@@ -182,16 +182,6 @@ def _step(q, kv_cache, block_table, context_lens):
     return B, _queries(q, B, dev), nb, Hkv, stride, index
 
 
-def _rows(shape, device, stream):
-    """Memory for a result, of the stream that writes it: the earlier work on it is
-    that stream's too, and it goes back there when it is dropped."""
-    torch = _torch()
-    if stream is None:
-        return torch.empty(shape, dtype=torch.float16, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=torch.float16, device=device)
-
-
 def _workspace(workspace, device):
     if not (_on(workspace, _torch().uint8, device.index) and workspace.is_contiguous()):
         _require(workspace, "workspace", _torch().uint8, device)
@@ -247,11 +237,11 @@ def gather(kv_cache, slot_mapping, k_out=None, v_out=None, stream=None):
     _want(slot_mapping, "slot_mapping", torch.int64, (T,), dev, index)
     shape = (T, Hkv, HEAD_DIM)
     if k_out is None:
-        k_out = _rows(shape, dev, stream)
+        k_out = _result(shape, dev, stream)
     else:
         _want(k_out, "k_out", torch.float16, shape, dev, index)
     if v_out is None:
-        v_out = torch.empty_like(k_out) if stream is None else _rows(shape, dev, stream)
+        v_out = torch.empty_like(k_out) if stream is None else _result(shape, dev, stream)
     else:
         _want(v_out, "v_out", torch.float16, shape, dev, index)
     _call("apex_kv4_gather", index, kv_cache.data_ptr(), slot_mapping.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
@@ -268,7 +258,7 @@ def attention(q, kv_cache, block_table, context_lens, scale, out=None, lse_out=N
     torch = _torch()
     B, Hq, nb, Hkv, stride, index = _step(q, kv_cache, block_table, context_lens)
     if out is None:
-        out = torch.empty_like(q) if stream is None else _rows(q.shape, q.device, stream)
+        out = torch.empty_like(q) if stream is None else _result(q.shape, q.device, stream)
     else:
         _want(out, "out", torch.float16, q.shape, q.device, index)
     if lse_out is not None:

@@ -51,3 +51,20 @@ def test_kv4_attention(torch, kv4):  # noqa: F811
     dq, dc, dt, dl = dev(torch, np.repeat(q, B, 0), cache, np.repeat(table, B, 0), np.repeat(lens, B))
     ws = torch.zeros(kv4.attention_workspace_bytes(B, 8, 1), dtype=torch.uint8, device="cuda")
     check_pool(torch, lambda s: [kv4.attention(dq, dc, dt, dl, 0.1, workspace=ws, stream=s)])
+
+
+@pytest.fixture(scope="module")
+def apex():
+    import paper_2506_03296_amd as A
+    A.load_library()
+    return A
+
+
+@pytest.mark.parametrize("name", ["decode_attention", "decode_attention_ex"])
+def test_decode_attention(torch, apex, name):  # noqa: F811
+    B = 9000
+    q = torch.randn((1, 8, 128), device="cuda").half().repeat(B, 1, 1)
+    k, v = (torch.randn((2, 1, BS, 128), device="cuda").half() for _ in range(2))
+    bt = torch.tensor([[1, 0]], dtype=torch.int32, device="cuda").repeat(B, 1)
+    lens = torch.full((B,), 20, dtype=torch.int32, device="cuda")
+    check_pool(torch, lambda s: [getattr(apex, name)(q, k, v, bt, lens, 0.1, stream=s)])
