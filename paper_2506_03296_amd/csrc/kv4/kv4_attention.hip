@@ -1131,11 +1131,12 @@ int apex_kv4_attention(const void* q, const void* kv_cache, const int32_t* block
     if (rc != APEX_OK) return rc;
     const size_t cb = counter_bytes(B, Hkv), pb = partial_bytes(cus);
     void *partials = workspace, *counters = (char*)workspace + pb;
+    kv4::Hold hold;
     if (workspace) {
         rc = kv4::check_workspace(workspace, workspace_bytes, pb + cb);
     } else {
-        rc = kv4::library_buffer(kv4::kCounters, cb, (hipStream_t)stream, &counters);
-        if (rc == APEX_OK) rc = kv4::library_buffer(kv4::kPartials, pb, (hipStream_t)stream, &partials);
+        rc = kv4::library_buffer(kv4::kCounters, cb, (hipStream_t)stream, hold, &counters);
+        if (rc == APEX_OK) rc = kv4::library_buffer(kv4::kPartials, pb, (hipStream_t)stream, hold, &partials);
     }
     if (rc != APEX_OK) return rc;
     Params p = fill(q, kv_cache, block_table, block_table_stride, context_lens, B, Hq, Hkv, num_blocks, scale, cus);

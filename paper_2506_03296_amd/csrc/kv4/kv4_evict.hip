@@ -814,8 +814,9 @@ extern "C" int apex_kv4_evict(void* kv_cache, const int32_t* block_table, int64_
     for (int i = 2; i < 6; ++i)
         if ((rc = check_disjoint(in[i], in, i)) != APEX_OK) return rc;
     const size_t need = need_bytes(B, Hkv, block_table_stride);
+    Hold hold;
     rc = workspace ? check_workspace(workspace, workspace_bytes, need)
-                   : library_buffer(kMasks, need, (hipStream_t)stream, &workspace);
+                   : library_buffer(kMasks, need, (hipStream_t)stream, hold, &workspace);
     if (rc != APEX_OK) return rc;
     int cus = 0;
     rc = compute_units(&cus);

@@ -1,8 +1,6 @@
 // kv4_host.cpp -- argument checks and workspaces of libapex_kv4.so.
 #include "kv4_host.h"
 
-#include <mutex>
-
 namespace kv4 {
 
 namespace {
@@ -12,8 +10,9 @@ struct Buffer {
     size_t bytes = 0;
 };
 
-std::mutex g_mutex;
+std::mutex g_mutex;         // of the buffers
 Buffer g_buffers[kMaxDevices][kLibraryBuffers];
+std::mutex g_units_mutex;
 int g_units[kMaxDevices];
 
 int current_device(int* dev)
@@ -72,7 +71,7 @@ int check_workspace(const void* given, size_t given_bytes, size_t bytes)
     return APEX_OK;
 }
 
-int library_buffer(LibraryBuffer kind, size_t bytes, hipStream_t stream, void** out)
+int library_buffer(LibraryBuffer kind, size_t bytes, hipStream_t stream, Hold& hold, void** out)
 {
     hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
     hipError_t e = hipStreamIsCapturing(stream, &st);
@@ -83,7 +82,7 @@ int library_buffer(LibraryBuffer kind, size_t bytes, hipStream_t stream, void** 
     int dev = 0;
     const int rc = current_device(&dev);
     if (rc != APEX_OK) return rc;
-    std::lock_guard<std::mutex> lock(g_mutex);
+    if (!hold) hold = Hold(g_mutex);
     Buffer& w = g_buffers[dev][kind];
     if (w.bytes < bytes) {
         if (w.ptr) {
@@ -119,7 +118,7 @@ int compute_units(int* out)
     int dev = 0;
     const int rc = current_device(&dev);
     if (rc != APEX_OK) return rc;
-    std::lock_guard<std::mutex> lock(g_mutex);
+    std::lock_guard<std::mutex> lock(g_units_mutex);
     if (g_units[dev] == 0) {
         int n = 0;
         hipError_t e = hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev);

@@ -6,6 +6,8 @@
 #include <limits.h>
 #include <stdint.h>
 
+#include <mutex>
+
 #include "apex_kv4.h"
 #include "kv4_format.h"
 #include "status.h"
@@ -49,8 +51,12 @@ int check_workspace(const void* given, size_t given_bytes, size_t bytes);
 // One of the library's own buffers on the current device, at least `bytes`
 // long; counters are zero when they are allocated.  Under stream capture it is
 // refused: a graph would keep an address that a later call may free.
+// The caller holds the buffers (`hold`, locked here) until it has launched what
+// uses them: another thread's call that grows or releases them waits for what has
+// been launched, and frees them then.
 enum LibraryBuffer { kCounters = 0, kPartials = 1, kMasks = 2, kLibraryBuffers = 3 };
-int library_buffer(LibraryBuffer kind, size_t bytes, hipStream_t stream, void** out);
+typedef std::unique_lock<std::mutex> Hold;
+int library_buffer(LibraryBuffer kind, size_t bytes, hipStream_t stream, Hold& hold, void** out);
 
 // Compute units of the current device.
 int compute_units(int* out);
