@@ -343,6 +343,9 @@ int enqueue(const apex_decode_args& a, bool noalloc)
     void* counters = nullptr;
     void* partials = nullptr;
     void* part_ml = nullptr;
+    // held, where the library's own buffers are used, until the launch: another
+    // thread's call that grows or releases them then waits for what was launched
+    std::unique_lock<std::mutex> hold(g_mutex, std::defer_lock);
     if (noalloc) {
         char* base = nullptr;
         rc = scratch_for(dev, (hipStream_t)a.stream, &base);
@@ -358,7 +361,7 @@ int enqueue(const apex_decode_args& a, bool noalloc)
         counters = a.workspace;
         partials = (char*)a.workspace + cbytes;
     } else {
-        std::lock_guard<std::mutex> lock(g_mutex);
+        hold.lock();
         DeviceState& s = g_dev[dev];
         rc = grow(s.counters, cbytes, true);
         if (rc != APEX_OK) return rc;
@@ -369,7 +372,7 @@ int enqueue(const apex_decode_args& a, bool noalloc)
     }
     void* error_word = nullptr;
     if (check) {
-        std::lock_guard<std::mutex> lock(g_mutex);
+        if (!hold) hold.lock();
         rc = grow(g_dev[dev].error_word, 4, true);
         if (rc != APEX_OK) return rc;
         error_word = g_dev[dev].error_word.ptr;
@@ -404,7 +407,7 @@ int enqueue(const apex_decode_args& a, bool noalloc)
     p.v_store = (apex::f16*)a.v_cache;
 #ifdef APEX_TRACE_WORK_GROUPS
     {
-        std::lock_guard<std::mutex> lock(g_mutex);
+        if (!hold) hold.lock();
         p.trace = g_trace;
         p.trace_groups = g_trace_groups;
     }

@@ -26,7 +26,8 @@ def program(tmp_path_factory):
 
 
 @pytest.mark.parametrize("other", ["grow", "release"])
-@pytest.mark.parametrize("lib,call", [("libapex_kv4.so", "attention"), ("libapex_kv4.so", "evict")])
+@pytest.mark.parametrize("lib,call", [("libapex_kv4.so", "attention"), ("libapex_kv4.so", "evict"),
+                                      ("libapex_decode.so", "decode")])
 def test_freed_after_the_launch(program, lib, call, other):
     r = subprocess.run([program, os.path.join(PACKAGE, lib), call, other], capture_output=True, text=True, timeout=60)
     assert r.returncode == 0, r.stdout + r.stderr
