@@ -249,8 +249,6 @@ def _result(shape, device, stream):
     """Memory for a result, of the stream that writes it: the earlier work on it is
     that stream's too, and it goes back there when it is dropped."""
     torch = _torch()
-    if stream is None:
-        return torch.empty(shape, dtype=torch.float16, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=torch.float16, device=device)
 
@@ -268,7 +266,8 @@ def decode_attention(q, k_cache, v_cache, block_table, context_lens, scale, out=
     ``decode_attention_ex`` for wider rows."""
     B, Hq, Hkv, d, bs, index = _dims(q, k_cache, v_cache, block_table, context_lens, out)
     if out is None:
-        out = _result((B, Hq, d), q.device, stream)
+        out = (_torch().empty((B, Hq, d), dtype=q.dtype, device=q.device) if stream is None
+               else _result((B, Hq, d), q.device, stream))
     rc = load_library().apex_decode_attention(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(),
         out.data_ptr(), B, Hq, Hkv, d, bs, ctypes.c_float(scale),
@@ -312,7 +311,8 @@ def decode_attention_ex(q, k_cache, v_cache, block_table, context_lens, scale, o
     torch = _torch()
     B, Hq, Hkv, d, bs, index = _dims(q, k_cache, v_cache, block_table, context_lens, out, block_table_stride)
     if out is None:
-        out = _result((B, Hq, d), q.device, stream)
+        out = (torch.empty((B, Hq, d), dtype=torch.float16, device=q.device) if stream is None
+               else _result((B, Hq, d), q.device, stream))
     if lse_out is not None and not (lse_out.shape == (B, Hq) and _on(lse_out, torch.float32, index)
                                     and lse_out.is_contiguous()):
         _require(lse_out, "lse_out", torch.float32, q.device, shape=(B, Hq))

@@ -237,7 +237,7 @@ def gather(kv_cache, slot_mapping, k_out=None, v_out=None, stream=None):
     _want(slot_mapping, "slot_mapping", torch.int64, (T,), dev, index)
     shape = (T, Hkv, HEAD_DIM)
     if k_out is None:
-        k_out = _result(shape, dev, stream)
+        k_out = torch.empty(shape, dtype=torch.float16, device=dev) if stream is None else _result(shape, dev, stream)
     else:
         _want(k_out, "k_out", torch.float16, shape, dev, index)
     if v_out is None:
