@@ -32,9 +32,10 @@
  * [B][block_table_stride]; a context longer than its table row is cut to the
  * row; entries past ceil(L_b / 16) are never read.  Block ids outside [0,
  * num_blocks) are skipped: their tokens take no part.  Supported: d = 128,
- * block_size = 16, Hq / Hkv in {1, 2, 4, 8}, B * Hkv * (block_table_stride + 64)
- * < 2^31, ceil(T / 16) * Hkv < 2^24, and in an eviction B * Hkv < 2^22 and
- * block_table_stride < 2^24; anything else returns APEX_ERR_UNSUPPORTED.
+ * block_size = 16, Hq / Hkv in {1, 2, 4, 8}, num_blocks < 2^31, block_table_stride < 2^27 - 1,
+ * B * Hkv * (block_table_stride + 64) < 2^31, ceil(T / 16) * Hkv < 2^24, and in an
+ * eviction B * Hkv < 2^22 and block_table_stride < 2^24; anything else returns
+ * APEX_ERR_UNSUPPORTED.
  *
  * Ownership and errors as in apex_decode.h: the caller owns every buffer, a
  * call validates on the host, enqueues its kernels on `stream` (NULL = the

@@ -57,8 +57,9 @@ int check_batch(int B, int Hq, int Hkv, int d, int block_size, int64_t num_block
     if (G != 1 && G != 2 && G != 4 && G != 8)
         return fail(APEX_ERR_UNSUPPORTED, "group size Hq/Hkv = %d unsupported (1, 2, 4, 8)", G);
     if (block_table_stride < 0) return fail(APEX_ERR_INVALID_ARG, "block_table_stride is negative");
-    if (block_table_stride >= INT_MAX / kBlockSize ||
-        (int64_t)B * Hkv > (int64_t)INT_MAX / (block_table_stride + 64))
+    if (block_table_stride >= INT_MAX / kBlockSize)
+        return fail(APEX_ERR_UNSUPPORTED, "block_table_stride %lld reaches 2^27 - 1", (long long)block_table_stride);
+    if ((int64_t)B * Hkv > (int64_t)INT_MAX / (block_table_stride + 64))
         return fail(APEX_ERR_UNSUPPORTED, "B * Hkv * (block_table_stride + 64) exceeds 2^31 - 1");
     return APEX_OK;
 }
