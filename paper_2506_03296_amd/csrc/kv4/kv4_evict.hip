@@ -474,16 +474,14 @@ __device__ inline int select_pair(const EvictParams& p, const int32_t* row, int 
     // the keep-th key from the top, digit by digit: candidates have key >> shift
     // == prefix.  Should more than kFew have the whole key, the same for their
     // slots, inverted: last_slot >> slot_shift of the candidates
-    unsigned prefix = 0, slots = 0;
-    int shift = 32, slot_shift = 32;   // (32: no digit yet)
+    static_assert(kN * kT > kFew, "a walk has more slots than are ranked");
+    unsigned prefix = find_digit([](unsigned, int) -> bool { return true; }, [](unsigned key, int) -> unsigned { return key >> 21; }, std::true_type());
+    unsigned slots = 0;
+    int shift = 21, slot_shift = 32;   // (32: no digit of the slots yet)
     auto in_keys = [&](unsigned key, int) -> bool { return key >> shift == prefix; };
     auto in_slots = [&](unsigned key, int t) -> bool {
         return key == prefix && (slot_shift == 32 || ~(unsigned)t >> slot_shift == slots);
     };
-    if (candidates > kFew) {
-        prefix = find_digit([](unsigned, int) -> bool { return true; }, [](unsigned key, int) -> unsigned { return key >> 21; }, std::true_type());
-        shift = 21;
-    }
     while (candidates > kFew && shift > 0) {
         const int to = shift == 21 ? 10 : 0;
         const unsigned dm = to == 0 ? 1023u : 2047u;
@@ -502,7 +500,7 @@ __device__ inline int select_pair(const EvictParams& p, const int32_t* row, int 
     if (tid == 0) sh.few_n = 0;
     __syncthreads();
     walk([&](unsigned key, int t, int) {
-        const bool c = shift == 32 || (slot_shift < 32 ? in_slots(key, t) : in_keys(key, t));
+        const bool c = slot_shift < 32 ? in_slots(key, t) : in_keys(key, t);
         if (c) sh.few[atomicAdd(&sh.few_n, 1)] = (uint64_t)key << 32 | ~(unsigned)t;
     }, no_batch);
     __syncthreads();
