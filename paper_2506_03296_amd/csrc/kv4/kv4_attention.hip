@@ -24,8 +24,10 @@
 // the token's weight at its own parity and zero at the other.  That saves the
 // byte permutes that a transpose in registers takes.  bf16 holds every
 // value of the cache exactly (fp16 would not hold the largest); the fp32
-// weights go in as two bf16 parts, 16 bits, in columns of their own (G = 8: in
-// two passes), while the normaliser sums them unrounded.
+// weights go in as two bf16 parts, in columns of their own (G = 8: in two passes):
+// the first cut off, the rest rounded to nearest, so that a weight is within 2^-16
+// of itself, to either side (the result's fp16 half step is 2^-11), while the
+// normaliser sums them unrounded.
 //
 // Bound by HBM for long batches: 32 requests of 4096-32768 tokens, 8 kv-heads, G =
 // 4, 452 MB in 79 us (5.7 TB/s; plain reads of slabs in the same pattern reach 6.8),
@@ -507,7 +509,7 @@ __device__ inline void attend(const Params& p, const Span& s, int lane, Pipe& pi
     const int parity = G == 8 ? col >> 3 : (col >> 2) & 1;
     // bytes 2 and 3 of a weight to the half of its parity, zeros to the other
     const unsigned place = parity ? 0x03020c0cu : 0x0c0c0302u;
-    const unsigned low_part = G < 8 && col >= 8 ? 0xffff0000u : 0u;
+    const unsigned low_part = G < 8 && col >= 8 ? 0xffff0000u : 0u, round = G == 8 || col >= 8 ? 0x8000u : 0u;
     st.m = -INFINITY;
     st.l = 0.f;
 #pragma unroll
@@ -579,11 +581,11 @@ __device__ inline void attend(const Params& p, const Span& s, int lane, Pipe& pi
                 const float we = w[4 * i + e];
                 const unsigned u = __float_as_uint(we);
                 if (G < 8) {
-                    const unsigned part = __float_as_uint(we - __uint_as_float(u & low_part));
+                    const unsigned part = __float_as_uint(we - __uint_as_float(u & low_part)) + round;
                     hi[e] = __builtin_amdgcn_perm(0u, part, place);
                 } else {
                     hi[e] = __builtin_amdgcn_perm(0u, u, place);
-                    lo[e] = __builtin_amdgcn_perm(0u, __float_as_uint(we - __uint_as_float(u & 0xffff0000u)), place);
+                    lo[e] = __builtin_amdgcn_perm(0u, __float_as_uint(we - __uint_as_float(u & 0xffff0000u)) + round, place);
                 }
             }
             const unsigned vs = x.t[i].vs;
