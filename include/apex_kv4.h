@@ -91,8 +91,9 @@ int apex_kv4_gather(const void* kv_cache, const int64_t* slot_mapping, void* k_o
  * (of values that an append rounded up) is 65504.
  * workspace: device memory of apex_kv4_attention_workspace_bytes bytes, 256-byte
  * aligned, all zero before its first call (calls of any shapes that it is large
- * enough for may follow; what they need zero they leave zero), or NULL for the
- * library's own, one per device, grown on demand (growing waits for the device).
+ * enough for may follow; what they need zero they leave zero, which an eviction
+ * does not), or NULL for the library's own, one per device, grown on demand (growing
+ * waits for the device).
  * Calls that can overlap need a workspace each, and so do a captured graph's
  * calls: under stream capture NULL is refused.
  */

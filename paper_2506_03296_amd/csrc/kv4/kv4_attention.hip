@@ -31,9 +31,9 @@
 //
 // Bound by HBM for long batches: 32 requests of 4096-32768 tokens, 8 kv-heads, G =
 // 4, 452 MB in 79 us (5.7 TB/s; plain reads of slabs in the same pattern reach 6.8),
-// one of 131071, 143 MB, in 29.2.  The difference is the launch, the first round trip
+// one of 131071, 143 MB, in 29.4.  The difference is the launch, the first round trip
 // (table, then slabs), the waves' uneven ends and the joining of split pairs, 6-8 us
-// a call, which is most of a small batch's time (16 of 256-4096, 38 MB, 15.9 us).
+// a call, which is most of a small batch's time (16 of 256-4096, 38 MB, 16.1 us).
 #include <type_traits>
 
 #include "kernels.h"

@@ -21,11 +21,12 @@
 // itself unless ids before it are outside the pool), and up to there such a slot's
 // bit says "kept", so that nothing is moved to it.
 //
-// 256 pairs of 2048-32768 tokens cut to 4096 take 154 us: 38 to select (8 bytes a
-// token, but three digits' counts, each with its barriers), 100 to move.  A row's
+// 256 pairs of 2048-32768 tokens cut to 4096 take 139 us: 39 to select (8 bytes a
+// token, but three digits' counts, each with its barriers), 99 to move.  A row's
 // values are 4-byte pieces over 256 bytes that it shares with three other tokens,
-// so the moves read 230 MB and write 126 for 190 MB of rows, 3.5 TB/s (a large copy
-// has 4.5).  Short pairs are bound by the launch and some ten round trips.
+// so the moves read 230 MB and write 126 for 190 MB of rows, 3.6 TB/s (a large copy
+// has 4.5).  Short pairs are bound by the launch and some ten round trips (128 of
+// 1025-1088 tokens cut to 1024: 14 us).
 #include <type_traits>
 
 #include "kernels.h"
@@ -316,9 +317,10 @@ __device__ inline void find_need(const int (&c)[kPer], int need, Digit<kT>& sh)
 template <int kT>
 struct Select {
     // counts of a digit, in copies by the lane's number: weights have few leading
-    // digits, and additions to one address wait for each other.  (First digit of a
-    // pair of 4664 tokens: 6.3 us with one copy, 3.2 with four; but of 1056 tokens
-    // with 256 threads, who clear and add up the copies, 2.1 and 3.9.)
+    // digits, and additions to one address wait for each other.  (256 pairs of
+    // 2048-32768 tokens, 1024 threads: selected in 45.1 us with one copy, 39.2 with
+    // two, 39.1 with four, which take twice the LDS; 128 of 1025-1088 with 256
+    // threads, who clear and add up the copies, 13.3 us with one and 14.0 with two.)
     static constexpr int kCopies = kT == kLarge ? 2 : 1;
     unsigned bins[kBins][kCopies];
     uint64_t few[kFew];

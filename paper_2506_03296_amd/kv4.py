@@ -254,7 +254,7 @@ def attention(q, kv_cache, block_table, context_lens, scale, out=None, lse_out=N
 
     ``workspace`` is an optional uint8 tensor of attention_workspace_bytes(B,
     Hq, Hkv) bytes or more, made by torch.zeros (calls of other shapes may share
-    it); calls that can overlap, and a captured graph, need one of their own."""
+    it, an eviction may not); calls that can overlap, and a captured graph, need one of their own."""
     torch = _torch()
     B, Hq, nb, Hkv, stride, index = _step(q, kv_cache, block_table, context_lens)
     if out is None:
