@@ -79,13 +79,14 @@ def test_evict(torch, kv4, kind, lens, keep, sinks, recent, entries):  # noqa: F
 
 
 # lengths for every number of tokens that a thread holds, for work groups of either
-# size, for one that reads its tokens again, and for pairs spread over work groups
+# size, for those that read their tokens again, and for pairs spread over work groups
 @pytest.mark.gpu
 @pytest.mark.parametrize("share", [0.02, 0.5, 0.97])
 @pytest.mark.parametrize("lens,Hkv,keep", [
     ([500, 33], 2, 200), ([2000, 400, 0], 2, 700), ([4000, 2049], 1, 1500), ([8000, 7000], 1, 6000),
     ([2000, 8200], 1, 900), ([16000, 9000], 1, 4096), ([32768, 17000], 1, 15000), ([9000] + [5] * 1030, 1, 3000),
-    ([33000, 700], 1, 20000), ([40960, 33333, 8192], 1, 8192)], ids=str)
+    ([33000, 700], 1, 20000), ([40960, 33333, 8192], 1, 8192), ([33333] + [40] * 70, 1, 20000)],
+                         ids=lambda x: str(x)[:24])
 def test_evict_of_lengths(torch, kv4, lens, Hkv, keep, share):  # noqa: F811
     cache, table, lens, w, pos = evict_case(lens, Hkv, seed=keep, kind="ties" if share == 0.5 else "normal")
     rng = np.random.default_rng(keep)
@@ -121,3 +122,30 @@ def test_attention_afterwards(torch, kv4, lens, keep):  # noqa: F811
     # weights 2^-15; half an fp16 step
     tol = (2 * 0.09 * np.abs(k).sum(-1).max() * 8 * 2.0 ** -18 + 2.0 ** -15) * np.abs(v).max() + np.abs(want) * 2.0 ** -11
     assert np.all(np.abs(out[0] - want) <= tol)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens,keep", [([3000, 60], 1000), ([33001, 700], 20000)], ids=str)
+def test_captured_and_replayed(torch, kv4, lens, keep):  # noqa: F811
+    """Rows with and without ids outside the pool by turns, in one graph."""
+    states = []
+    for share in (0.0, 0.3, 0.0, 0.9):
+        cache, table, lens_, w, pos = evict_case(lens, 2, seed=len(states))
+        rng = np.random.default_rng(len(states))
+        lose(cache, table, lens_, [np.flatnonzero(rng.random(-(-L // BS)) < share) for L in lens])
+        first = [torch.from_numpy(x).cuda() for x in (cache, table, w, pos)]
+        O.evict(cache, table, lens_, w, pos, keep, 4, keep // 4)
+        states.append((first, (cache, w, pos)))
+    buf = [x.clone() for x in states[0][0]]
+    dl = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ws = torch.full((kv4.evict_workspace_bytes(len(lens), 2, buf[1].shape[1]),), 255, dtype=torch.uint8, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=s):
+        kv4.evict(buf[0], buf[1], dl, buf[2], buf[3], keep, 4, keep // 4, workspace=ws)
+    for first, want in states + states:
+        for x, y in zip(buf, first):
+            x.copy_(y)
+        g.replay()
+        assert same([buf[i].cpu().numpy() for i in (0, 2, 3)], want)
