@@ -22,6 +22,11 @@ KV4_DIR = os.path.join(CSRC, "kv4")
 KV4_SOURCES = [os.path.join(KV4_DIR, "kv4_rows.hip"), os.path.join(KV4_DIR, "kv4_attention.hip"),
                os.path.join(KV4_DIR, "kv4_evict.hip"), os.path.join(KV4_DIR, "kv4_host.cpp"),
                os.path.join(CSRC, "status.cpp")]
+STEPS_LIB = os.path.join(HERE, "libapex_steps.so")
+STEPS_DIR = os.path.join(CSRC, "steps")
+STEPS_SOURCES = [os.path.join(STEPS_DIR, "steps_blocks.hip"), os.path.join(STEPS_DIR, "prompt_attention.hip"),
+                 os.path.join(STEPS_DIR, "tree_attention.hip"), os.path.join(STEPS_DIR, "steps_host.cpp"),
+                 os.path.join(CSRC, "status.cpp")]
 HEADERS = [os.path.join(ROOT, "include", "apex_decode.h"),
            os.path.join(ROOT, "include", "apex_kv_append.h"),
            os.path.join(ROOT, "include", "apex_decode_trace.h"),
@@ -83,10 +88,11 @@ def build(out=LIB, extra=(), quiet=False):
     """Compile the decode-attention library, its work-group trace build (the
     same sources with APEX_TRACE_WORK_GROUPS), the host attention backend,
     the overlap runtime (linked against the host backend), the HBM probe
-    library and the 4-bit KV cache."""
+    library, the 4-bit KV cache and the steps of several tokens a request."""
     build_cpu(quiet=quiet)
     _compile(PROBE_SOURCES, PROBE_LIB, extra, quiet)
     _compile(KV4_SOURCES, KV4_LIB, extra, quiet)
+    _compile(STEPS_SOURCES, STEPS_LIB, extra, quiet)
     _compile(SOURCES, TRACE_LIB, [*extra, "-DAPEX_TRACE_WORK_GROUPS"], quiet)
     _compile(OVERLAP_SOURCES, OVERLAP_LIB,
              [*extra, "-L", HERE, "-lapex_cpu", "-Wl,-rpath,$ORIGIN", "-pthread"], quiet)

@@ -1,0 +1,325 @@
+// attend_tile.h -- one wave's part of an attention: 32 query rows against tiles
+// of keys that lie in LDS.
+//
+// A wave keeps 32 rows of q and their 32 x 128 sums in registers and takes the
+// keys as they come, with the running maximum and sum of a softmax in one pass:
+//     S^T = K Q^T          (keys down, queries across: v_mfma_f32_32x32x16_f16)
+//     p   = 2^(c s - M)    (c = |scale| log2 e, M at most 2^kSlack below the row's maximum)
+//     O^T += V^T P^T
+// Transposed, a query is a lane's column in all three products: its maximum,
+// sum and rescaling need no broadcast, only one exchange between the wave's
+// halves (lanes n and n + 32 hold the same query's other keys).  The weights
+// leave S^T in the order in which P^T takes them, but for the naming of the 16
+// keys of a step; V^T is read in that naming too, so they stay where they are.
+//
+// Rounding: scores, maxima, sums and O are fp32.  The weights enter the second
+// product as fp16 (half a step: 2^-12 of a weight, at random), which the output's
+// own rounding to fp16 matches; they are 2^kBias times what the softmax defines,
+// so that weights down to 2^-(24 + kBias) of the largest one still count.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace steps __attribute__((visibility("hidden"))) {
+
+constexpr int kHeadDim = 128;
+constexpr int kBlockSize = 16;
+constexpr int kWaveRows = 32;      // query rows of a wave
+constexpr int kRowBytes = kHeadDim * 2;
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// M follows the running maximum only when that has passed it by 2^kSlack: the
+// sums are rescaled on few tiles.  2^(kBias + kSlack) is an fp16 value.
+constexpr float kSlack = 8.0f;
+constexpr float kBias = 7.0f;
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) f16x8 lds_f16x8;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+
+// Where 16-byte piece c of a key's row lies among the row's 16 pieces.  K is
+// read with 32 neighbouring keys at one piece each: their pieces are spread over
+// all banks.  V is read, transposed, as 4 neighbouring keys at four pieces each
+// (64 bytes): each key's go to another quarter.
+__device__ inline unsigned k_piece(unsigned key, unsigned c) { return c ^ (key & 15); }
+__device__ inline unsigned v_piece(unsigned key, unsigned c) { return c ^ ((key & 3) << 2); }
+
+// x of this lane and of the lane 32 away, in either order.
+__device__ inline u32x2 both_halves(float x)
+{
+    const unsigned u = __float_as_uint(x);
+    return __builtin_amdgcn_permlane32_swap(u, u, false, false);
+}
+
+__device__ inline float max_of_halves(float x)
+{
+    const u32x2 r = both_halves(x);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ inline float sum_of_halves(float x)
+{
+    const u32x2 r = both_halves(x);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A row of zeros, for rows that are not there.
+__device__ __attribute__((aligned(16))) const unsigned int kZeros[kRowBytes / 4] = {0};
+
+// 16 bytes of every lane from global memory to LDS, lane i's to `to` + 16 i (`to`
+// the same in all lanes), past the registers; done when the wave has waited for
+// its loads (arrived).
+__device__ inline void load_to_lds(const char* from, unsigned to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+}
+
+// Waits until all but the last n of the wave's loads have arrived and what it has
+// read from LDS is there.
+template <int n>
+__device__ inline void arrived()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(n) : "memory");
+}
+
+// Waits for the work group; LDS before it is LDS behind it.
+__device__ inline void barrier()
+{
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+__device__ inline unsigned lds_address(const lds_char* p) { return (unsigned)(uintptr_t)p; }
+
+// One wave's rows: kSub tiles of 32 keys are taken at a time.
+template <int kSub>
+struct Rows {
+    f16x8 q[8];          // lane n and n + 32: row n, dims 16 s + 8 (lane / 32) + 0..7 in q[s]
+    f32x16 o[4];         // O^T, dims 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4 in o[t][i], times 2^kBias
+    float top;           // M
+    float sum;           // of this lane's half of the keys
+
+    // Row pointer of the lane's query, or NULL: a row of zeros.  A negative
+    // scale is taken as its magnitude, with q's sign turned.
+    __device__ void start(const char* row, bool negate)
+    {
+        const unsigned half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            u32x4 x = {0u, 0u, 0u, 0u};
+            if (row) x = *(const u32x4*)(row + s * 32 + half * 16);
+            if (negate) x ^= 0x80008000u;
+            q[s] = __builtin_bit_cast(f16x8, x);
+        }
+        clear();
+    }
+
+    __device__ void clear()
+    {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+        top = -INFINITY;
+        sum = 0.0f;
+    }
+
+    // Scores of the tiles' keys: key 32 u + 8 (i / 4) + 4 (lane / 32) + i % 4 in s[u][i].
+    __device__ void scores(const lds_char* k, f32x16 (&s)[kSub]) const
+    {
+        const unsigned lane = threadIdx.x & 63, key = lane & 31, half = lane >> 5;
+#pragma unroll
+        for (int u = 0; u < kSub; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const unsigned at = key * kRowBytes + k_piece(key, 2 * j + half) * 16;
+#pragma unroll
+            for (int u = 0; u < kSub; ++u) {
+                const f16x8 a = *(const lds_f16x8*)(k + at + u * 32 * kRowBytes);
+                s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[j], s[u], 0, 0, 0);
+            }
+        }
+    }
+
+    // Takes out the scores of keys that the lane's query does not see: bit j of
+    // `allow` stands for key j.
+    __device__ static void mask(f32x16 (&s)[kSub], uint64_t allow)
+    {
+        const unsigned half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+        for (int u = 0; u < kSub; ++u) {
+            const uint32_t bits = (uint32_t)(allow >> (32 * u)) >> (4 * half);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                s[u][i] = (bits >> (8 * (i / 4) + i % 4)) & 1 ? s[u][i] : -INFINITY;
+        }
+    }
+
+    // Weights of the scores, as P^T's operands: keys 16 w + 4 half + 0..3 and + 8 in p[w].
+    __device__ void weights(const f32x16 (&s)[kSub], float c, f16x8 (&p)[2 * kSub])
+    {
+        float m = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < kSub; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m = fmaxf(m, s[u][i]);
+        m = max_of_halves(m) * c;
+        if (__builtin_expect(__any(m > top + kSlack), 0)) rescale(fmaxf(m, top));
+        // a row that has seen no score yet keeps M = -inf: 2^(-inf - 0) = 0
+        const float base = (top == -INFINITY ? 0.0f : top) - kBias;
+        float part = 0.0f;
+#pragma unroll
+        for (int u = 0; u < kSub; ++u)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {
+                    f32x2 e;
+                    e[0] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][8 * w + j], c, -base));
+                    e[1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][8 * w + j + 1], c, -base));
+                    part += e[0];
+                    part += e[1];
+                    const f16x2 h = __builtin_convertvector(e, f16x2);
+                    p[2 * u + w][j] = h[0];
+                    p[2 * u + w][j + 1] = h[1];
+                }
+            }
+        sum += part;
+    }
+
+    __device__ void rescale(float to)
+    {
+        const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - to);
+        sum *= f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] *= f;
+        top = to;
+    }
+
+    // V^T's operand: dims 32 t + lane % 32, the 16 keys of step w in P^T's order.
+    __device__ static f16x8 v_operand(const lds_char* v, int w, int t)
+    {
+        const unsigned lane = threadIdx.x & 63, half = lane >> 5, in = lane & 15;
+        const unsigned key = 4 * half + (in >> 2), quarter = (unsigned)t ^ (in >> 2);
+        const unsigned at = key * kRowBytes + quarter * 64 + ((lane >> 4) & 1) * 32 + (in & 3) * 8;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v + at + w * 16 * kRowBytes));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v + at + (w * 16 + 8) * kRowBytes));
+        return __builtin_bit_cast(f16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+
+    __device__ void add(const lds_char* v, const f16x8 (&p)[2 * kSub])
+    {
+#pragma unroll
+        for (int w = 0; w < 2 * kSub; ++w)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_operand(v, w, t), p[w], o[t], 0, 0, 0);
+    }
+
+    // True if some sum of the wave's is an infinity or a NaN.  That need not be the
+    // rows' own: a masked key has the weight 0, but 0 x NaN is NaN.  The wave then
+    // clears its sums and takes its keys anew, one by one.
+    __device__ bool spoiled() const
+    {
+        float x = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x += o[t][i];
+        return __any(!(fabsf(x) < INFINITY));
+    }
+
+    // One key, by its rows in global memory (this kv-head's), for the queries that see it.
+    __device__ void take_key(const char* k, const char* v, float c, bool sees)
+    {
+        const unsigned half = (threadIdx.x & 63) >> 5;
+        float dot = 0.0f;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const f16x8 x = *(const f16x8*)(k + s * 32 + half * 16);
+#pragma unroll
+            for (int j = 0; j < 8; j += 2)
+                dot = __builtin_amdgcn_fdot2(f16x2{x[j], x[j + 1]}, f16x2{q[s][j], q[s][j + 1]}, dot, false);
+            asm volatile("" ::: "memory");      // one load at a time: this path may not cost the other registers
+        }
+        dot = sum_of_halves(dot);
+        const float m = sees ? dot * c : -INFINITY;
+        if (__any(m > top + kSlack)) rescale(fmaxf(m, top));
+        const float base = (top == -INFINITY ? 0.0f : top) - kBias;
+        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, c, -base));
+        if (!sees) return;
+        if (half == 0) sum += e;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f16x4 x = *(const f16x4*)(v + t * 64 + i * 16 + half * 8);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[t][4 * i + j] = __builtin_fmaf(e, (float)x[j], o[t][4 * i + j]);
+                asm volatile("" ::: "memory");
+            }
+    }
+};
+
+// The index of a call's rows: row r of a request is head r % G of its token r / G.
+struct Group {
+    int heads;       // q-heads of a kv-head (G)
+    __device__ void split(unsigned row, unsigned* token, unsigned* head) const
+    {
+        *token = row / (unsigned)heads;
+        *head = row - *token * (unsigned)heads;
+    }
+};
+
+// A value that is the same in all lanes, as the compiler cannot know.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+}
+
+// Sum over a wave's lanes.
+__device__ inline int wave_sum(int x)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
+    return uniform(x);
+}
+
+// Largest of a wave's lanes.
+__device__ inline int wave_max(int x)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) x = max(x, __shfl_xor(x, m));
+    return uniform(x);
+}
+
+// Inclusive sums over a wave's lanes.
+__device__ inline int wave_scan(int x)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const int y = __shfl_up(x, m);
+        if (lane >= m) x += y;
+    }
+    return x;
+}
+
+}  // namespace steps
