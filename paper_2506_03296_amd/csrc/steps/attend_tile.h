@@ -95,6 +95,9 @@ __device__ inline void arrived()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(n) : "memory");
 }
 
+// Waits until what the wave has read from LDS is there: loads may overwrite it.
+__device__ inline void was_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // Waits for the work group; LDS before it is LDS behind it.
 __device__ inline void barrier()
 {

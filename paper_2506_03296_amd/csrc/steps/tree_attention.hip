@@ -7,7 +7,6 @@ namespace steps {
 
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kSlabBytes = kBlockSize * kRowBytes;
 
 // A pair is one request, one kv-head and one tile of its rows.  Its keys are taken
@@ -59,17 +58,22 @@ __device__ inline int request_cost(const TreeArgs& a, const Request& r)
 
 // kRowTiles waves hold a tile of rows each, kWaves / kRowTiles waves share a row
 // tile's keys, 32 kSub each of a unit.
-template <int kRowTiles, int kSub>
-__global__ __launch_bounds__(kThreads, kRowTiles == 1 ? 1 : 2) void tree_kernel(TreeArgs a)
+template <int kRowTiles, int kSub, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
 {
     constexpr int kParts = kWaves / kRowTiles;
     constexpr int kWaveKeys = 32 * kSub, kKeys = kParts * kWaveKeys;
     constexpr int kTileRows = kRowTiles * kWaveRows;
-    constexpr bool kOwn = kRowTiles == 1;                // a wave brings the keys that it takes, and no others
-    constexpr int kLoads = kKeys / 16;                   // of K, and of V, by which a wave brings its share of a unit
+    // A wave brings the keys that it takes and no others, into one buffer of its own
+    // (kOwn), or the work group's waves bring a unit together, into one of two.
+    constexpr bool kOwn = kRowTiles == 1;
+    constexpr int kBuffers = kOwn ? 1 : 2;
+    constexpr int kLoads = kKeys / (4 * kWaves);         // of K, and of V, by which a wave brings its share of a unit
+    constexpr int kBlocks = kOwn ? kWaveKeys / kBlockSize : kKeys / kBlockSize;    // in which this share lies
     constexpr int kBytes = kKeys * kRowBytes;            // of K or of V
-    static_assert(kParts == 1 || kWaves * kWaveRows * kHeadDim * 4 <= 4 * kBytes, "the sums pass through the buffers");
-    __shared__ __attribute__((aligned(16))) char lds[2 * 2 * kBytes];
+    static_assert(kParts == 1 || kWaves * kWaveRows * kHeadDim * 4 <= 2 * kBuffers * kBytes, "the sums pass through the buffers");
+    static_assert(kOwn || kWaves == 4, "a wave's load brings four of a block's 16 keys");
+    __shared__ __attribute__((aligned(16))) char lds[2 * kBuffers * kBytes];
     __shared__ float merge_top[kWaves][kWaveRows], merge_sum[kWaves][kWaveRows];
 
     const unsigned lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -136,59 +140,60 @@ __global__ __launch_bounds__(kThreads, kRowTiles == 1 ? 1 : 2) void tree_kernel(
         const int32_t* ids = a.table + (int64_t)b * a.table_stride;
 
         // A unit's rows: load j of a wave brings four keys, in LDS one behind the
-        // other, and lane i the piece that belongs at i % 16 of key i / 16.  There are
-        // two buffers: a unit is on its way while the one before it is worked on.
-        unsigned there = 0, there_next = 0;              // blocks of this wave's loads that are in the pool
-        const auto load = [&](int u) {
-            const unsigned to = lds_address(shared) + (u & 1) * 2 * kBytes;
-            const char *k[kLoads], *v[kLoads];
-            there_next = 0;
+        // other, and lane i the piece that belongs at i % 16 of key i / 16.  The ids of
+        // the blocks are asked for a unit ahead.
+        int ids_next[kBlocks];
+        const auto ask = [&](int u) {
+#pragma unroll
+            for (int j = 0; j < kBlocks; ++j) {
+                const int e = u * (kKeys / kBlockSize) + (kOwn ? (int)wave * kBlocks : 0) + j;
+                ids_next[j] = u < cached && e * kBlockSize < q.len ? ids[e] : -1;
+            }
+        };
+        unsigned there_next = 0;                         // blocks of ids_next that are in the pool
+        const auto load = [&](int u, const char* cache, const char* fresh, bool is_v) {
+            const unsigned to = lds_address(shared) + (u & (kBuffers - 1)) * 2 * kBytes + (is_v ? kBytes : 0);
             const int left = u < cached ? q.len - u * kKeys : q.nodes;
+            there_next = 0;
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
                 const int first_key = kOwn ? (int)wave * kWaveKeys + j * 4 : j * 16 + (int)wave * 4;
                 const int key = first_key + (int)(lane >> 4), block = kOwn ? j / 4 : j;
+                const unsigned piece = is_v ? v_piece(key, lane & 15) : k_piece(key, lane & 15);
+                const char* from;
                 if (u < cached) {
-                    const int e = u * (kKeys / kBlockSize) + first_key / kBlockSize;
-                    const int id = e * kBlockSize < q.len ? ids[e] : -1;
+                    const int id = ids_next[block];
                     const bool in_pool = id >= 0 && id < (int)a.num_blocks;
                     if (in_pool) there_next |= 1u << block;
-                    const int64_t slab = ((int64_t)id * a.Hkv + kv_head) * kSlabBytes + (key % kBlockSize) * kRowBytes;
-                    k[j] = a.k_cache + slab + k_piece(key, lane & 15) * 16;
-                    v[j] = a.v_cache + slab + v_piece(key, lane & 15) * 16;
-                    if (!in_pool || key >= left) k[j] = v[j] = (const char*)kZeros;
+                    from = cache + ((int64_t)id * a.Hkv + kv_head) * kSlabBytes + (key % kBlockSize) * kRowBytes + piece * 16;
+                    if (!in_pool || key >= left) from = (const char*)kZeros;
                 } else {
-                    const int64_t row = (int64_t)(q.first + key) * a.new_stride + kv_head * kRowBytes;
-                    k[j] = a.k_new + row + k_piece(key, lane & 15) * 16;
-                    v[j] = a.v_new + row + v_piece(key, lane & 15) * 16;
-                    if (key >= left) k[j] = v[j] = (const char*)kZeros;
+                    from = fresh + (int64_t)(q.first + key) * a.new_stride + kv_head * kRowBytes + piece * 16;
+                    if (key >= left) from = (const char*)kZeros;
                 }
+                load_to_lds(from, to + first_key * kRowBytes);
             }
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j)
-                load_to_lds(k[j], to + (kOwn ? wave * kWaveKeys + j * 4 : j * 16 + wave * 4) * kRowBytes);
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j)
-                load_to_lds(v[j], to + kBytes + (kOwn ? wave * kWaveKeys + j * 4 : j * 16 + wave * 4) * kRowBytes);
         };
+        const auto load_k = [&](int u) { load(u, a.k_cache, a.k_new, false); };
+        const auto load_v = [&](int u) { load(u, a.v_cache, a.v_new, true); };
         const int from = part * kWaveKeys;               // this wave's keys of a unit
+        ask(lo);
         barrier();                                       // the buffers are free
-        load(lo);
+        load_k(lo);
+        load_v(lo);
         for (int u = lo; u < hi; ++u) {
-            there = there_next;
+            const unsigned there = there_next;
+            const bool more = u + 1 < hi;
+            if (more) ask(u + 1);
             if (kOwn) {
-                // its own loads are all that the wave waits for, K's first
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                if (u + 1 < hi) {
-                    load(u + 1);
-                    arrived<3 * kLoads>();
-                } else {
-                    arrived<kLoads>();
-                }
+                arrived<kLoads>();                       // K
             } else {
                 arrived<0>();
                 barrier();
-                if (u + 1 < hi) load(u + 1);
+                if (more) {
+                    load_k(u + 1);
+                    load_v(u + 1);
+                }
             }
             uint64_t allow;                              // the keys that the lane's row sees
             bool all = false;
@@ -203,17 +208,25 @@ __global__ __launch_bounds__(kThreads, kRowTiles == 1 ? 1 : 2) void tree_kernel(
             } else {
                 allow = from < 64 ? tree >> from : 0;
             }
-            const lds_char* kt = shared + (u & 1) * 2 * kBytes + from * kRowBytes;
+            const lds_char* kt = shared + (u & (kBuffers - 1)) * 2 * kBytes + from * kRowBytes;
             f32x16 s[kSub];
             f16x8 p[2 * kSub];
             r.scores(kt, s);
+            if (kOwn && more) {
+                was_read();
+                load_k(u + 1);
+            }
             if (!all) r.mask(s, allow);
             r.weights(s, a.c, p);
             if (kOwn) {
-                if (u + 1 < hi) arrived<2 * kLoads>();
+                if (more) arrived<kLoads>();             // V; the next K is on its way
                 else arrived<0>();
             }
             r.add(kt + kBytes, p);
+            if (kOwn && more) {
+                was_read();
+                load_v(u + 1);
+            }
         }
         if (__builtin_expect(r.spoiled(), 0)) {
             r.clear();
@@ -281,9 +294,9 @@ __global__ __launch_bounds__(kThreads, kRowTiles == 1 ? 1 : 2) void tree_kernel(
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            if (kParts > 1 && t / (4 / kParts) != part) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
+                if (kParts > 1 && (t * 4 + i) / (16 / kParts) != part) continue;
                 f32x4 y = {r.o[t][4 * i], r.o[t][4 * i + 1], r.o[t][4 * i + 2], r.o[t][4 * i + 3]};
                 if (kParts > 1) {
                     y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -488,8 +501,8 @@ int apex_steps_tree_attention(const void* q, int64_t q_token_stride, const void*
     a.G = G;
     a.c = (scale < 0 ? -scale : scale) * kLog2e;
     a.negate = scale < 0;
-    const auto kernel = waves == 1 ? tree_kernel<1, 1> : waves == 2 ? tree_kernel<2, 1> : tree_kernel<4, 2>;
-    kernel<<<groups, kThreads, 0, (hipStream_t)stream>>>(a);
+    const auto kernel = waves == 1 ? tree_kernel<1, 1, 8> : waves == 2 ? tree_kernel<2, 1, 4> : tree_kernel<4, 2, 4>;
+    kernel<<<groups, waves == 1 ? 512 : 256, 0, (hipStream_t)stream>>>(a);
     rc = launched("tree_attention");
     if (rc != APEX_OK) return rc;
     join_kernel<<<dim3(groups, tile_rows / 8), 256, 0, (hipStream_t)stream>>>(a, tile_rows);
