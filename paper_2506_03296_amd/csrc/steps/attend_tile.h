@@ -48,7 +48,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) f16x8 lds_f16x8;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 
 // Where 16-byte piece c of a key's row lies among the row's 16 pieces.  K is
 // read with 32 neighbouring keys at one piece each: their pieces are spread over
@@ -87,6 +87,12 @@ __device__ inline void load_to_lds(const char* from, unsigned to)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
 }
 
+// The same from one address in all lanes and an offset of each.
+__device__ inline void load_to_lds(const char* from, unsigned offset, unsigned to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(from) : "memory");
+}
+
 // Waits until all but the last n of the wave's loads have arrived and what it has
 // read from LDS is there.
 template <int n>
@@ -106,56 +112,72 @@ __device__ inline void barrier()
 
 __device__ inline unsigned lds_address(const lds_char* p) { return (unsigned)(uintptr_t)p; }
 
-// One wave's rows: kSub tiles of 32 keys are taken at a time.
-template <int kSub>
+// One wave's rows, kTiles tiles of 32; kSub tiles of 32 keys are taken at a time.
+template <int kSub, int kTiles = 1>
 struct Rows {
-    f16x8 q[8];          // lane n and n + 32: row n, dims 16 s + 8 (lane / 32) + 0..7 in q[s]
-    f32x16 o[4];         // O^T, dims 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4 in o[t][i], times 2^kBias
-    float top;           // M
-    float sum;           // of this lane's half of the keys
+    f16x8 q[kTiles][8];      // lane n and n + 32: row n, dims 16 j + 8 (lane / 32) + 0..7 in q[][j]
+    f32x16 o[kTiles][4];     // O^T, dims 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4 in o[][t][i], times 2^kBias
+    float top[kTiles];       // M
+    float sum[kTiles];       // of this lane's half of the keys
 
-    // Row pointer of the lane's query, or NULL: a row of zeros.  A negative
-    // scale is taken as its magnitude, with q's sign turned.
-    __device__ void start(const char* row, bool negate)
+    // Row pointer of the lane's query of tile r, or NULL: a row of zeros.
+    __device__ void start(int r, const char* row)
     {
         const unsigned half = (threadIdx.x & 63) >> 5;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
+        for (int j = 0; j < 8; ++j) {
             u32x4 x = {0u, 0u, 0u, 0u};
-            if (row) x = *(const u32x4*)(row + s * 32 + half * 16);
-            if (negate) x ^= 0x80008000u;
-            q[s] = __builtin_bit_cast(f16x8, x);
+            if (row) x = *(const u32x4*)(row + j * 32 + half * 16);
+            q[r][j] = __builtin_bit_cast(f16x8, x);
         }
-        clear();
+    }
+
+    // A negative scale is taken as its magnitude, with q's sign turned.
+    __device__ void negate()
+    {
+#pragma unroll
+        for (int r = 0; r < kTiles; ++r)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[r][j] = __builtin_bit_cast(f16x8, __builtin_bit_cast(u32x4, q[r][j]) ^ 0x80008000u);
     }
 
     __device__ void clear()
     {
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int r = 0; r < kTiles; ++r) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
-        top = -INFINITY;
-        sum = 0.0f;
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[r][t][i] = 0.0f;
+            top[r] = -INFINITY;
+            sum[r] = 0.0f;
+        }
     }
 
-    // Scores of the tiles' keys: key 32 u + 8 (i / 4) + 4 (lane / 32) + i % 4 in s[u][i].
-    __device__ void scores(const lds_char* k, f32x16 (&s)[kSub]) const
+    // Scores of the tiles' keys: key 32 u + 8 (i / 4) + 4 (lane / 32) + i % 4 in s[][u][i].
+    __device__ void scores(const lds_char* k, f32x16 (&s)[kTiles][kSub]) const
     {
         const unsigned lane = threadIdx.x & 63, key = lane & 31, half = lane >> 5;
+        f16x8 a[kSub][8];
 #pragma unroll
         for (int u = 0; u < kSub; ++u)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
+            for (int j = 0; j < 8; ++j)
+                a[u][j] = *(const lds_f16x8*)(k + (key + 32 * u) * kRowBytes + k_piece(key, 2 * j + half) * 16);
+        __builtin_amdgcn_sched_barrier(0);      // all reads are on their way before the first product waits
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const unsigned at = key * kRowBytes + k_piece(key, 2 * j + half) * 16;
+        for (int r = 0; r < kTiles; ++r)
 #pragma unroll
-            for (int u = 0; u < kSub; ++u) {
-                const f16x8 a = *(const lds_f16x8*)(k + at + u * 32 * kRowBytes);
-                s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, q[j], s[u], 0, 0, 0);
-            }
-        }
+            for (int u = 0; u < kSub; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[r][u][i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int u = 0; u < kSub; ++u)
+#pragma unroll
+                for (int r = 0; r < kTiles; ++r)
+                    s[r][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][j], q[r][j], s[r][u], 0, 0, 0);
     }
 
     // Takes out the scores of keys that the lane's query does not see: bit j of
@@ -172,8 +194,8 @@ struct Rows {
         }
     }
 
-    // Weights of the scores, as P^T's operands: keys 16 w + 4 half + 0..3 and + 8 in p[w].
-    __device__ void weights(const f32x16 (&s)[kSub], float c, f16x8 (&p)[2 * kSub])
+    // Weights of tile r's scores, as P^T's operands: keys 16 w + 4 half + 0..3 and + 8 in p[w].
+    __device__ void weights(int r, const f32x16 (&s)[kSub], float c, f16x8 (&p)[2 * kSub])
     {
         float m = -INFINITY;
 #pragma unroll
@@ -181,9 +203,9 @@ struct Rows {
 #pragma unroll
             for (int i = 0; i < 16; ++i) m = fmaxf(m, s[u][i]);
         m = max_of_halves(m) * c;
-        if (__builtin_expect(__any(m > top + kSlack), 0)) rescale(fmaxf(m, top));
+        if (__builtin_expect(__any(m > top[r] + kSlack), 0)) rescale(r, fmaxf(m, top[r]));
         // a row that has seen no score yet keeps M = -inf: 2^(-inf - 0) = 0
-        const float base = (top == -INFINITY ? 0.0f : top) - kBias;
+        const float base = (top[r] == -INFINITY ? 0.0f : top[r]) - kBias;
         float part = 0.0f;
 #pragma unroll
         for (int u = 0; u < kSub; ++u)
@@ -201,18 +223,18 @@ struct Rows {
                     p[2 * u + w][j + 1] = h[1];
                 }
             }
-        sum += part;
+        sum[r] += part;
     }
 
-    __device__ void rescale(float to)
+    __device__ void rescale(int r, float to)
     {
-        const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - to);
-        sum *= f;
+        const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top[r] - to);
+        sum[r] *= f;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[t][i] *= f;
-        top = to;
+            for (int i = 0; i < 16; ++i) o[r][t][i] *= f;
+        top[r] = to;
     }
 
     // V^T's operand: dims 32 t + lane % 32, the 16 keys of step w in P^T's order.
@@ -226,13 +248,37 @@ struct Rows {
         return __builtin_bit_cast(f16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 
-    __device__ void add(const lds_char* v, const f16x8 (&p)[2 * kSub])
+    // The operands of `n` steps from step w on.
+    template <int n>
+    __device__ static void read_v(const lds_char* v, int w, f16x8 (&a)[n][4])
     {
 #pragma unroll
-        for (int w = 0; w < 2 * kSub; ++w)
+        for (int i = 0; i < n; ++i)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) a[i][t] = v_operand(v, w + i, t);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+
+    template <int n>
+    __device__ void add(int w, const f16x8 (&a)[n][4], const f16x8 (&p)[kTiles][2 * kSub])
+    {
+#pragma unroll
+        for (int i = 0; i < n; ++i)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_operand(v, w, t), p[w], o[t], 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < kTiles; ++r)
+                    o[r][t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][t], p[r][w + i], o[r][t], 0, 0, 0);
+    }
+
+    __device__ void add(const lds_char* v, const f16x8 (&p)[kTiles][2 * kSub])
+    {
+#pragma unroll
+        for (int w = 0; w < 2 * kSub; w += 2) {
+            f16x8 a[2][4];
+            read_v(v, w, a);
+            add(w, a, p);
+        }
     }
 
     // True if some sum of the wave's is an infinity or a NaN.  That need not be the
@@ -242,39 +288,41 @@ struct Rows {
     {
         float x = 0.0f;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int r = 0; r < kTiles; ++r)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x += o[t][i];
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x += o[r][t][i];
         return __any(!(fabsf(x) < INFINITY));
     }
 
-    // One key, by its rows in global memory (this kv-head's), for the queries that see it.
-    __device__ void take_key(const char* k, const char* v, float c, bool sees)
+    // One key, by its rows in global memory (this kv-head's), for the queries of tile r that see it.
+    __device__ void take_key(int r, const char* k, const char* v, float c, bool sees)
     {
         const unsigned half = (threadIdx.x & 63) >> 5;
         float dot = 0.0f;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
-            const f16x8 x = *(const f16x8*)(k + s * 32 + half * 16);
+        for (int j = 0; j < 8; ++j) {
+            const f16x8 x = *(const f16x8*)(k + j * 32 + half * 16);
 #pragma unroll
-            for (int j = 0; j < 8; j += 2)
-                dot = __builtin_amdgcn_fdot2(f16x2{x[j], x[j + 1]}, f16x2{q[s][j], q[s][j + 1]}, dot, false);
+            for (int i = 0; i < 8; i += 2)
+                dot = __builtin_amdgcn_fdot2(f16x2{x[i], x[i + 1]}, f16x2{q[r][j][i], q[r][j][i + 1]}, dot, false);
             asm volatile("" ::: "memory");      // one load at a time: this path may not cost the other registers
         }
         dot = sum_of_halves(dot);
         const float m = sees ? dot * c : -INFINITY;
-        if (__any(m > top + kSlack)) rescale(fmaxf(m, top));
-        const float base = (top == -INFINITY ? 0.0f : top) - kBias;
+        if (__any(m > top[r] + kSlack)) rescale(r, fmaxf(m, top[r]));
+        const float base = (top[r] == -INFINITY ? 0.0f : top[r]) - kBias;
         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, c, -base));
         if (!sees) return;
-        if (half == 0) sum += e;
+        if (half == 0) sum[r] += e;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const f16x4 x = *(const f16x4*)(v + t * 64 + i * 16 + half * 8);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o[t][4 * i + j] = __builtin_fmaf(e, (float)x[j], o[t][4 * i + j]);
+                for (int j = 0; j < 4; ++j) o[r][t][4 * i + j] = __builtin_fmaf(e, (float)x[j], o[r][t][4 * i + j]);
                 asm volatile("" ::: "memory");
             }
     }

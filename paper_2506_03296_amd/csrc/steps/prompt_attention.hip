@@ -108,7 +108,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
     const int tiles = all_hi / kKeys + 1, own_tiles = wave_live ? wave_hi / kKeys + 1 : 0;
 
     Rows<2> r;
-    r.start(live ? a.q + (int64_t)(first + (int)pos) * a.q_stride + qhead * kRowBytes : nullptr, a.negate);
+    r.start(0, live ? a.q + (int64_t)(first + (int)pos) * a.q_stride + qhead * kRowBytes : nullptr);
+    if (a.negate) r.negate();
+    r.clear();
 
     // A tile's rows: load j of a wave brings four keys, in LDS one behind the other,
     // and lane i the piece that belongs at i % 16 of key i / 16.  There are two
@@ -137,14 +139,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
         barrier();
         if (t + 1 < tiles) load(t + 1);
         const lds_char* kt = shared + (t & 1) * 2 * kTileBytes;
-        f32x16 s[2];
-        f16x8 p[4];
+        f32x16 s[1][2];
+        f16x8 p[1][4];
         r.scores(kt, s);
         if ((t + 1) * kKeys > wave_lo + 1) {
             const int seen = (int)pos - t * kKeys + 1;      // keys of the tile up to the row's own
-            r.mask(s, seen >= 64 ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
+            r.mask(s[0], seen >= 64 ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
         }
-        r.weights(s, a.c, p);
+        r.weights(0, s[0], a.c, p[0]);
         r.add(kt + kTileBytes, p);
     }
     for (; t < tiles; ++t) {     // tiles that only other waves see
@@ -157,11 +159,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
 #pragma nounroll
         for (int key = 0; key <= wave_hi; ++key) {
             const int64_t at = request0 + (int64_t)key * a.kv_stride;
-            r.take_key(a.k + at, a.v + at, a.c, key <= (int)pos);
+            r.take_key(0, a.k + at, a.v + at, a.c, key <= (int)pos);
         }
     }
 
-    const float sum = sum_of_halves(r.sum);
+    const float sum = sum_of_halves(r.sum[0]);
     if (!live) return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int64_t at = (int64_t)(first + (int)pos) * a.Hq + qhead;
@@ -170,10 +172,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            f32x4 x = {r.o[t][4 * i] * inv, r.o[t][4 * i + 1] * inv, r.o[t][4 * i + 2] * inv, r.o[t][4 * i + 3] * inv};
+            f32x4 x = {r.o[0][t][4 * i] * inv, r.o[0][t][4 * i + 1] * inv, r.o[0][t][4 * i + 2] * inv, r.o[0][t][4 * i + 3] * inv};
             *(f16x4*)(a.out + at * kRowBytes + t * 64 + i * 16 + half * 8) = __builtin_convertvector(x, f16x4);
         }
-    if (a.lse && half == 0) a.lse[at] = (r.top - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
+    if (a.lse && half == 0) a.lse[at] = (r.top[0] - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 }  // namespace

@@ -32,13 +32,23 @@ struct TreeArgs {
     bool negate;
 };
 
+// The kernel's arguments, read again: what only the ends of a part need does not
+// stay in registers between them.
+using Arguments = const __attribute__((address_space(4))) TreeArgs*;
+__device__ inline Arguments arguments()
+{
+    Arguments p = (Arguments)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
 struct Request {
     int first, nodes, len;         // its first packed row, its drafted and its cached tokens
     int units, tiles;              // units of a pair, tiles of rows
 };
 
-template <int kTileRows, int kKeys>
-__device__ inline Request read_request(const TreeArgs& a, int b)
+template <int kTileRows, int kKeys, class Args>
+__device__ inline Request read_request(const Args& a, int b)
 {
     Request r;
     const int lo = min(max(a.offsets[b], 0), a.T), hi = min(max(a.offsets[b + 1], lo), a.T);
@@ -51,54 +61,75 @@ __device__ inline Request read_request(const TreeArgs& a, int b)
 }
 
 // Units of all of a request's pairs.
-__device__ inline int request_cost(const TreeArgs& a, const Request& r)
+template <class Args>
+__device__ inline int request_cost(const Args& a, const Request& r)
 {
     return r.nodes ? a.Hkv * r.tiles * (r.units + kPairCost) : 0;
 }
 
-// kRowTiles waves hold a tile of rows each, kWaves / kRowTiles waves share a row
-// tile's keys, 32 kSub each of a unit.
-template <int kRowTiles, int kSub, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
+// kRowWaves waves hold kTiles tiles of 32 rows each, kWaves / kRowWaves waves share
+// their keys, 32 kSub each of a unit.
+template <int kTiles_, int kRowWaves_, int kSub_, int kWaves_>
+struct Shape {
+    static constexpr int kTiles = kTiles_, kRowWaves = kRowWaves_, kSub = kSub_, kWaves = kWaves_;
+    static constexpr int kParts = kWaves / kRowWaves;
+    static constexpr int kWaveKeys = 32 * kSub, kKeys = kParts * kWaveKeys;
+    static constexpr int kWaveTile = kTiles * kWaveRows, kTileRows = kRowWaves * kWaveTile;
+    static constexpr int kBytes = kKeys * kRowBytes;             // of a unit's K or V
+    // A wave brings the keys that it takes and no others, into one buffer, each half
+    // of which it fills again as soon as it has read it (kOwn), or the work group's
+    // waves bring a unit together, into one of two buffers.
+    static constexpr bool kOwn = kRowWaves == 1;
+    static constexpr int kBuffers = kOwn ? 1 : 2, kLds = 2 * kBuffers * kBytes;
+    static constexpr int kLoads = kKeys / (4 * kWaves);          // of K, and of V, by which a wave brings its share of a unit
+    static constexpr int kPartBlocks = kWaveKeys / kBlockSize;   // blocks of a wave's keys
+    // Parts' sums are joined by way of the buffer that the last unit has left (of
+    // kOwn its half for V), in rounds.
+    static constexpr int kRounds = kParts == 1 ? 1 : kWaves * kWaveTile * kHeadDim * 4 / ((kOwn ? 1 : 2) * kBytes);
+    static_assert(kParts == 1 || kRounds == 1 || kRounds == 2 || kRounds == 4, "a round takes 128 / kRounds dims");
+};
+
+// A part of a pair that a work group takes: units [lo, hi) of it.
+struct Segment {
+    Request q;
+    int b, pair_at, lo, hi, kv_head, tile, cached;
+};
+
+template <class S>
+__global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
 {
-    constexpr int kParts = kWaves / kRowTiles;
-    constexpr int kWaveKeys = 32 * kSub, kKeys = kParts * kWaveKeys;
-    constexpr int kTileRows = kRowTiles * kWaveRows;
-    // A wave brings the keys that it takes and no others, into one buffer of its own
-    // (kOwn), or the work group's waves bring a unit together, into one of two.
-    constexpr bool kOwn = kRowTiles == 1;
-    constexpr int kBuffers = kOwn ? 1 : 2;
-    constexpr int kLoads = kKeys / (4 * kWaves);         // of K, and of V, by which a wave brings its share of a unit
-    constexpr int kBlocks = kOwn ? kWaveKeys / kBlockSize : kKeys / kBlockSize;    // in which this share lies
-    constexpr int kBytes = kKeys * kRowBytes;            // of K or of V
-    static_assert(kParts == 1 || kWaves * kWaveRows * kHeadDim * 4 <= 2 * kBuffers * kBytes, "the sums pass through the buffers");
-    static_assert(kOwn || kWaves == 4, "a wave's load brings four of a block's 16 keys");
-    __shared__ __attribute__((aligned(16))) char lds[2 * kBuffers * kBytes];
-    __shared__ float merge_top[kWaves][kWaveRows], merge_sum[kWaves][kWaveRows];
+    constexpr int kTiles = S::kTiles, kParts = S::kParts, kWaveKeys = S::kWaveKeys, kKeys = S::kKeys, kLoads = S::kLoads;
+    constexpr int kTileRows = S::kTileRows, kBytes = S::kBytes, kSub = S::kSub;
+    constexpr bool kOwn = S::kOwn;
+    __shared__ __attribute__((aligned(16))) char lds[S::kLds];
+    __shared__ float merge_top[S::kWaves][S::kWaveTile], merge_sum[S::kWaves][S::kWaveTile];
 
-    const unsigned lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned lane = threadIdx.x & 63, wave = (unsigned)uniform((int)(threadIdx.x >> 6));
     const unsigned half = lane >> 5;
-    const int row_tile = (int)wave % kRowTiles, part = (int)wave / kRowTiles;
+    const int row_wave = (int)wave % S::kRowWaves, part = (int)wave / S::kRowWaves;
+    const int from = part * kWaveKeys;                   // this wave's keys of a unit
 
-    // the share of this work group
-    int64_t total = 0;
-    for (int i = 0; i < a.B; i += 64) {
-        int cost = 0;
-        if (i + (int)lane < a.B) cost = request_cost(a, read_request<kTileRows, kKeys>(a, i + lane));
-        total += wave_sum(cost);
-    }
-    const int64_t active = min((int64_t)gridDim.x, (total + kLeastShare - 1) / kLeastShare);
+    // the share of this work group: [begin, end) of `total` units
     if (threadIdx.x == 0) a.joins[2 * blockIdx.x] = int4{0, 0, 0, 0};
-    if ((int64_t)blockIdx.x >= active) return;
-    const int64_t begin = uniform((int64_t)(total * blockIdx.x / active));
-    const int64_t end = uniform((int64_t)(total * (blockIdx.x + 1) / active));
+    Request mine = {};                                   // of request `lane`
+    if ((int)lane < a.B) mine = read_request<kTileRows, kKeys>(a, lane);
+    const int cost0 = request_cost(a, mine), upto0 = wave_scan(cost0);
+    int total = __builtin_amdgcn_readlane(upto0, 63);
+    for (int i = 64; i < a.B; i += 64)
+        total += wave_sum(i + (int)lane < a.B ? request_cost(a, read_request<kTileRows, kKeys>(a, i + lane)) : 0);
+    const int active = min((int)gridDim.x, (total + kLeastShare - 1) / kLeastShare);
+    if ((int)blockIdx.x >= active) return;
+    const int share = uniform(total / active), longer = total - share * active;      // the first `longer` take one more
+    const int begin = share * (int)blockIdx.x + min((int)blockIdx.x, longer);
+    const int end = begin + share + ((int)blockIdx.x < longer ? 1 : 0);
     // the request that `begin` falls into, and where its pairs start
-    int b = 0;
-    int64_t base = 0;
+    int b = 0, base = 0;
     for (int i = 0; i < a.B; i += 64) {
-        int cost = 0;
-        if (i + (int)lane < a.B) cost = request_cost(a, read_request<kTileRows, kKeys>(a, i + lane));
-        const int upto = wave_scan(cost);
+        int cost = cost0, upto = upto0;
+        if (i) {
+            cost = i + (int)lane < a.B ? request_cost(a, read_request<kTileRows, kKeys>(a, i + lane)) : 0;
+            upto = wave_scan(cost);
+        }
         const uint64_t behind = __ballot(base + upto > begin);
         if (behind) {
             const int l = __builtin_ctzll(behind);
@@ -111,222 +142,343 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
     b = uniform(b);
     base = uniform(base);
 
-    Rows<kSub> r;
-    lds_char* const shared = (lds_char*)lds;
-    for (int64_t x = begin; x < end;) {
-        Request q = read_request<kTileRows, kKeys>(a, b);
-        const int cost = request_cost(a, q);
-        if (x >= base + cost) {
-            base += cost;
-            ++b;
-            continue;
-        }
-        const int per_pair = q.units + kPairCost;
-        const int pair = uniform((int)((x - base) / per_pair));
-        const int64_t at = base + (int64_t)pair * per_pair + kPairCost;      // the pair's unit 0
-        const int lo = (int)max(x - at, (int64_t)0), hi = (int)min(end - at, (int64_t)q.units);
-        x = at + q.units;
-        if (hi <= lo) continue;
-        const int kv_head = pair / q.tiles, tile = pair - kv_head * q.tiles;
-        const int cached = q.units - 1;                  // units of cached tokens
-        const int rows = min(kTileRows, q.nodes * a.G - tile * kTileRows);
-
-        const unsigned row = (unsigned)(tile * kTileRows + row_tile * kWaveRows) + (lane & 31);
-        const bool live = (int)row < q.nodes * a.G;
-        const unsigned node = min(row / (unsigned)a.G, (unsigned)q.nodes - 1);
-        const unsigned qhead = (unsigned)kv_head * a.G + row % (unsigned)a.G;
-        r.start(live ? a.q + (int64_t)(q.first + (int)node) * a.q_stride + qhead * kRowBytes : nullptr, a.negate);
-        const uint64_t tree = a.mask[q.first + (int)node] & (q.nodes >= 64 ? ~0ull : (1ull << q.nodes) - 1);
-        const int32_t* ids = a.table + (int64_t)b * a.table_stride;
-
-        // A unit's rows: load j of a wave brings four keys, in LDS one behind the
-        // other, and lane i the piece that belongs at i % 16 of key i / 16.  The ids of
-        // the blocks are asked for a unit ahead.
-        int ids_next[kBlocks];
-        const auto ask = [&](int u) {
-#pragma unroll
-            for (int j = 0; j < kBlocks; ++j) {
-                const int e = u * (kKeys / kBlockSize) + (kOwn ? (int)wave * kBlocks : 0) + j;
-                ids_next[j] = u < cached && e * kBlockSize < q.len ? ids[e] : -1;
+    int x = begin;
+    const auto next = [&](Segment& g) {                  // false: there are no more
+        const Arguments f = arguments();
+        while (x < end) {
+            if (b < 64) {
+                g.q.first = __builtin_amdgcn_readlane(mine.first, b);
+                g.q.nodes = __builtin_amdgcn_readlane(mine.nodes, b);
+                g.q.len = __builtin_amdgcn_readlane(mine.len, b);
+                g.q.units = __builtin_amdgcn_readlane(mine.units, b);
+                g.q.tiles = __builtin_amdgcn_readlane(mine.tiles, b);
+            } else {
+                g.q = read_request<kTileRows, kKeys>(*f, b);
             }
-        };
-        unsigned there_next = 0;                         // blocks of ids_next that are in the pool
-        const auto load = [&](int u, const char* cache, const char* fresh, bool is_v) {
-            const unsigned to = lds_address(shared) + (u & (kBuffers - 1)) * 2 * kBytes + (is_v ? kBytes : 0);
-            const int left = u < cached ? q.len - u * kKeys : q.nodes;
-            there_next = 0;
+            const int cost = request_cost(*f, g.q);
+            if (x >= base + cost) {
+                base += cost;
+                ++b;
+                continue;
+            }
+            const int per_pair = g.q.units + kPairCost;
+            const int pair = uniform((x - base) / per_pair);
+            g.b = b;
+            g.pair_at = base + pair * per_pair + kPairCost;      // the pair's unit 0
+            g.lo = max(x - g.pair_at, 0);
+            g.hi = min(end - g.pair_at, g.q.units);
+            g.kv_head = g.q.tiles == 1 ? pair : uniform(pair / g.q.tiles);
+            g.tile = pair - g.kv_head * g.q.tiles;
+            g.cached = g.q.units - 1;                    // units of cached tokens
+            x = g.pair_at + g.q.units;
+            if (g.hi > g.lo) return true;
+        }
+        return false;
+    };
+
+    // A unit's rows: load j of a wave brings four keys, in LDS one behind the other,
+    // and lane i the piece that belongs at i % 16 of key i / 16.
+    lds_char* const shared = (lds_char*)lds;
+    constexpr int kIds = kOwn ? kLoads / 4 : kLoads;
+    int ids[kIds], part_ids[S::kPartBlocks];             // of the blocks of the unit that is asked for next
+    const unsigned block_bytes = (unsigned)a.Hkv * kSlabBytes, num_blocks = (unsigned)a.num_blocks;
+    const auto first_key = [&](int j) { return kOwn ? (int)wave * kWaveKeys + j * 4 : (j * S::kWaves + (int)wave) * 4; };
+    const auto id_of = [&](const Segment& g, const int32_t* row, int u, int key) {
+        const int e = u * (kKeys / kBlockSize) + key / kBlockSize;
+        return u < g.cached && e * kBlockSize < g.q.len ? row[e] : -1;
+    };
+    const auto ask = [&](const Segment& g, int u) {
+        const Arguments f = arguments();
+        const int32_t* row = f->table + (int64_t)g.b * f->table_stride;
+#pragma unroll
+        for (int j = 0; j < kIds; ++j) ids[j] = id_of(g, row, u, first_key(kOwn ? 4 * j : j));
+#pragma unroll
+        for (int j = 0; j < S::kPartBlocks; ++j) part_ids[j] = id_of(g, row, u, from + j * kBlockSize);
+    };
+    const auto load = [&](const Segment& g, int u, int buffer, bool is_v) {
+        const Arguments f = arguments();
+        const char* const head = (is_v ? f->v_cache : f->k_cache) + (int64_t)g.kv_head * kSlabBytes;
+        const unsigned to = (unsigned)uniform((int)(lds_address(shared) + buffer * 2 * kBytes + (is_v ? kBytes : 0)));
+        const unsigned quad = lane >> 4;                 // the lane's key of a load's four
+        const int left = u < g.cached ? g.q.len - u * kKeys : g.q.nodes;
+        bool plain = first_key(kLoads - 1) + 4 <= left;
+#pragma unroll
+        for (int j = 0; j < kIds; ++j) plain = plain && (unsigned)ids[j] < num_blocks;
+        if (plain) {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
-                const int first_key = kOwn ? (int)wave * kWaveKeys + j * 4 : j * 16 + (int)wave * 4;
-                const int key = first_key + (int)(lane >> 4), block = kOwn ? j / 4 : j;
-                const unsigned piece = is_v ? v_piece(key, lane & 15) : k_piece(key, lane & 15);
-                const char* from;
-                if (u < cached) {
-                    const int id = ids_next[block];
-                    const bool in_pool = id >= 0 && id < (int)a.num_blocks;
-                    if (in_pool) there_next |= 1u << block;
-                    from = cache + ((int64_t)id * a.Hkv + kv_head) * kSlabBytes + (key % kBlockSize) * kRowBytes + piece * 16;
-                    if (!in_pool || key >= left) from = (const char*)kZeros;
-                } else {
-                    from = fresh + (int64_t)(q.first + key) * a.new_stride + kv_head * kRowBytes + piece * 16;
-                    if (key >= left) from = (const char*)kZeros;
-                }
-                load_to_lds(from, to + first_key * kRowBytes);
+                // of a block's 16 keys, the load's first
+                const unsigned in_block = kOwn ? (j & 3) * 4 : (wave & 3) * 4;
+                const unsigned offset = (in_block + quad) * kRowBytes
+                                        + (is_v ? v_piece(quad, lane & 15) : k_piece(in_block + quad, lane & 15)) * 16;
+                load_to_lds(head + (int64_t)ids[kOwn ? j / 4 : j] * block_bytes, offset, to + first_key(j) * kRowBytes);
             }
-        };
-        const auto load_k = [&](int u) { load(u, a.k_cache, a.k_new, false); };
-        const auto load_v = [&](int u) { load(u, a.v_cache, a.v_new, true); };
-        const int from = part * kWaveKeys;               // this wave's keys of a unit
-        ask(lo);
-        barrier();                                       // the buffers are free
-        load_k(lo);
-        load_v(lo);
-        for (int u = lo; u < hi; ++u) {
-            const unsigned there = there_next;
-            const bool more = u + 1 < hi;
-            if (more) ask(u + 1);
-            if (kOwn) {
-                arrived<kLoads>();                       // K
-            } else {
-                arrived<0>();
-                barrier();
-                if (more) {
-                    load_k(u + 1);
-                    load_v(u + 1);
-                }
+            return;
+        }
+        if (u >= g.cached) {                             // drafted tokens
+            const char* const fresh = (is_v ? f->v_new : f->k_new) + (int64_t)g.q.first * f->new_stride + g.kv_head * kRowBytes;
+#pragma nounroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int key = first_key(j) + (int)quad;
+                const char* row = fresh + key * f->new_stride + (is_v ? v_piece(key, lane & 15) : k_piece(key, lane & 15)) * 16;
+                if (key >= left) row = (const char*)kZeros;
+                load_to_lds(row, to + first_key(j) * kRowBytes);
             }
-            uint64_t allow;                              // the keys that the lane's row sees
-            bool all = false;
-            if (u < cached) {
-                allow = 0;
+            return;
+        }
 #pragma unroll
-                for (int j = 0; j < kWaveKeys / kBlockSize; ++j)
-                    if (there >> ((kOwn ? 0 : from / kBlockSize) + j) & 1) allow |= 0xffffull << (16 * j);
-                const int n = q.len - u * kKeys - from;
-                allow &= n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
-                all = allow == (kSub == 2 ? ~0ull : 0xffffffffull);
-            } else {
-                allow = from < 64 ? tree >> from : 0;
-            }
-            const lds_char* kt = shared + (u & (kBuffers - 1)) * 2 * kBytes + from * kRowBytes;
-            f32x16 s[kSub];
-            f16x8 p[2 * kSub];
-            r.scores(kt, s);
-            if (kOwn && more) {
-                was_read();
-                load_k(u + 1);
-            }
-            if (!all) r.mask(s, allow);
-            r.weights(s, a.c, p);
-            if (kOwn) {
-                if (more) arrived<kLoads>();             // V; the next K is on its way
-                else arrived<0>();
-            }
-            r.add(kt + kBytes, p);
-            if (kOwn && more) {
-                was_read();
-                load_v(u + 1);
+        for (int j = 0; j < kLoads; ++j) {               // a context's end, blocks outside the pool
+            const unsigned in_block = (kOwn ? (j & 3) * 4 : (wave & 3) * 4) + quad;
+            const int id = ids[kOwn ? j / 4 : j];
+            const char* row = head + (int64_t)id * block_bytes + in_block * kRowBytes
+                              + (is_v ? v_piece(quad, lane & 15) : k_piece(in_block, lane & 15)) * 16;
+            if ((unsigned)id >= num_blocks || first_key(j) + (int)quad >= left) row = (const char*)kZeros;
+            load_to_lds(row, to + first_key(j) * kRowBytes);
+        }
+    };
+    // which blocks of the wave's part are in the pool
+    const auto present = [&]() {
+        unsigned bits = 0;
+#pragma unroll
+        for (int j = 0; j < S::kPartBlocks; ++j)
+            if ((unsigned)part_ids[j] < num_blocks) bits |= 1u << j;
+        return bits;
+    };
+    Rows<kSub, kTiles> r;
+    uint64_t tree[kTiles];                               // the drafted tokens that the lane's rows see
+    const auto row_of = [&](const Segment& g, int i) {
+        return (unsigned)(g.tile * kTileRows + row_wave * S::kWaveTile + i * kWaveRows) + (lane & 31);
+    };
+    const auto rows = [&](const Segment& g, uint64_t (&words)[kTiles]) {
+        const Arguments f = arguments();
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) {
+            const unsigned row = row_of(g, i), G = (unsigned)f->G, node = row / G;
+            const bool live = (int)node < g.q.nodes;
+            r.start(i, live ? f->q + (int64_t)(g.q.first + (int)node) * f->q_stride + (g.kv_head * G + row - node * G) * kRowBytes
+                            : nullptr);
+            words[i] = live ? f->mask[g.q.first + (int)node] : 0;
+        }
+    };
+
+    Segment g, ahead;
+    if (!next(g)) return;
+    ask(g, g.lo);
+    rows(g, tree);
+    r.clear();
+    unsigned there = present(), buffer = 0;
+    load(g, g.lo, 0, false);
+    load(g, g.lo, 0, true);
+    if (a.negate) r.negate();
+    const float c = a.c;
+    for (int u = g.lo;;) {
+        // the unit that is brought while this one is worked on: the part's next, or
+        // the first of the work group's next part
+        const bool last = u + 1 == g.hi;
+        bool more = true;
+        if (last) more = next(ahead);
+        else ahead = g;
+        const int u_ahead = last ? ahead.lo : u + 1;
+        if (more) ask(ahead, u_ahead);
+        if (kOwn) {
+            arrived<kLoads>();                           // K
+        } else {
+            arrived<0>();
+            barrier();
+            if (more) {
+                load(ahead, u_ahead, buffer ^ 1, false);
+                load(ahead, u_ahead, buffer ^ 1, true);
             }
         }
-        if (__builtin_expect(r.spoiled(), 0)) {
-            r.clear();
-#pragma nounroll
-            for (int i = 0; i < (hi - lo) * kWaveKeys; ++i) {
-                const int u = lo + i / kWaveKeys, key = from + i % kWaveKeys;
-                const char *k = (const char*)kZeros, *v = k;
-                bool sees = false;
-                if (u < cached) {
-                    const int token = u * kKeys + key;
-                    const int id = token < q.len ? ids[token / kBlockSize] : -1;
-                    if (id >= 0 && id < (int)a.num_blocks) {
-                        const int64_t to = ((int64_t)id * a.Hkv + kv_head) * kSlabBytes + token % kBlockSize * kRowBytes;
-                        k = a.k_cache + to;
-                        v = a.v_cache + to;
-                        sees = true;
-                    }
-                } else if (key < q.nodes) {
-                    const int64_t to = (int64_t)(q.first + key) * a.new_stride + kv_head * kRowBytes;
-                    k = a.k_new + to;
-                    v = a.v_new + to;
-                    sees = tree >> key & 1;
-                }
-                r.take_key(k, v, a.c, sees);
+        lds_char* const kt = shared + (kOwn ? 0 : buffer * 2 * kBytes) + from * kRowBytes;
+        f32x16 s[kTiles][kSub];
+        f16x8 p[kTiles][2 * kSub];
+        r.scores(kt, s);
+        if (kOwn && more) {
+            was_read();
+            load(ahead, u_ahead, 0, false);
+        }
+        if (u < g.cached) {
+            uint64_t allow = 0;                          // the keys that are there
+#pragma unroll
+            for (int j = 0; j < S::kPartBlocks; ++j)
+                if (there >> j & 1) allow |= 0xffffull << (16 * j);
+            const int n = g.q.len - u * kKeys - from;
+            allow &= n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
+            if (allow != (kSub == 2 ? ~0ull : 0xffffffffull)) {
+#pragma unroll
+                for (int i = 0; i < kTiles; ++i) r.mask(s[i], allow);
             }
+        } else {
+            const uint64_t nodes = from >= 64 ? 0 : (g.q.nodes >= 64 ? ~0ull : (1ull << g.q.nodes) - 1) >> from;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) r.mask(s[i], tree[i] >> (from & 63) & nodes);
+        }
+        if (kOwn) {
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) r.weights(i, s[i], c, p[i]);
+            if (more) arrived<kLoads>();                 // V; the next K is on its way
+            else arrived<0>();
+            r.add(kt + kBytes, p);
+            if (!last) {
+                was_read();
+                load(ahead, u_ahead, 0, true);
+            }
+        } else {
+            // V's operands come while the weights are made
+            f16x8 v[2][4];
+            r.read_v(kt + kBytes, 0, v);
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) r.weights(i, s[i], c, p[i]);
+            r.add(0, v, p);
+            if (kSub == 2) {
+                r.read_v(kt + kBytes, 2, v);
+                r.add(2, v, p);
+            }
+        }
+        there = present();
+        if (!last) {
+            ++u;
+            buffer ^= 1;
+            continue;
         }
 
-        // the parts' sums together: each wave of a row tile joins some of the dims
-        float top = r.top, sum = sum_of_halves(r.sum), f[kParts];
-        f[0] = 1.0f;
+        // the part's end
+        const Arguments out = arguments();
+        if (__builtin_expect(r.spoiled(), 0)) {
+            r.clear();
+            const int32_t* row = out->table + (int64_t)g.b * out->table_stride;
+#pragma nounroll
+            for (int i = 0; i < (g.hi - g.lo) * kWaveKeys; ++i) {
+                const int v = g.lo + i / kWaveKeys, key = from + i % kWaveKeys;
+                const char *k_row = (const char*)kZeros, *v_row = k_row;
+                bool is_there = false;
+                if (v < g.cached) {
+                    const int id = v * kKeys + key < g.q.len ? id_of(g, row, v, key) : -1;
+                    if ((unsigned)id < num_blocks) {
+                        const int64_t to = (int64_t)id * block_bytes + (int64_t)g.kv_head * kSlabBytes + key % kBlockSize * kRowBytes;
+                        k_row = out->k_cache + to;
+                        v_row = out->v_cache + to;
+                        is_there = true;
+                    }
+                } else if (key < g.q.nodes) {
+                    const int64_t to = (int64_t)(g.q.first + key) * out->new_stride + g.kv_head * kRowBytes;
+                    k_row = out->k_new + to;
+                    v_row = out->v_new + to;
+                    is_there = true;
+                }
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j)
+                    r.take_key(j, k_row, v_row, c, is_there && (v < g.cached || (tree[j] >> (key & 63) & 1)));
+            }
+        }
+        if (more) rows(ahead, tree);                     // on their way while the parts meet
+
+        // the parts' sums together, each wave of a tile some of the dims
+        lds_char* const meet = shared + (kOwn ? kBytes : buffer * 2 * kBytes);
+        const bool whole = g.lo == 0 && g.hi == g.q.units;
+        const int64_t slot = 2 * (int64_t)blockIdx.x + (g.lo == 0 ? 1 : 0);
+        float top[kTiles], sum[kTiles], f[kTiles][kParts];
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) {
+            top[n] = r.top[n];
+            sum[n] = sum_of_halves(r.sum[n]);
+        }
         if (kParts > 1) {
+            if (half == 0) {
+#pragma unroll
+                for (int n = 0; n < kTiles; ++n) {
+                    merge_top[wave][n * kWaveRows + lane] = top[n];
+                    merge_sum[wave][n * kWaveRows + lane] = sum[n];
+                }
+            }
             barrier();
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int n = 0; n < kTiles; ++n) {
+                const int i = n * kWaveRows + (lane & 31);
+                top[n] = -INFINITY;
+                sum[n] = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *(__attribute__((address_space(3))) f32x4*)(shared + ((wave * 16 + t * 4 + i) * 64 + lane) * 16) =
-                        f32x4{r.o[t][4 * i], r.o[t][4 * i + 1], r.o[t][4 * i + 2], r.o[t][4 * i + 3]};
-            if (half == 0) {
-                merge_top[wave][lane] = top;
-                merge_sum[wave][lane] = sum;
-            }
-            __syncthreads();
-            float tp[kParts];
-            top = -INFINITY;
+                for (int w = 0; w < kParts; ++w) {
+                    f[n][w] = merge_top[w * S::kRowWaves + row_wave][i];
+                    top[n] = fmaxf(top[n], f[n][w]);
+                }
 #pragma unroll
-            for (int w = 0; w < kParts; ++w) {
-                tp[w] = merge_top[w * kRowTiles + row_tile][lane & 31];
-                top = fmaxf(top, tp[w]);
-            }
-            sum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kParts; ++w) {
-                f[w] = tp[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(tp[w] - top);
-                const float sw = merge_sum[w * kRowTiles + row_tile][lane & 31];
-                sum += f[w] * sw;
-                // a part's NaN stays one also where the part has seen no score
-                if (sw != sw) sum = sw;
+                for (int w = 0; w < kParts; ++w) {
+                    f[n][w] = f[n][w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(f[n][w] - top[n]);
+                    sum[n] = __builtin_fmaf(f[n][w], merge_sum[w * S::kRowWaves + row_wave][i], sum[n]);
+                }
             }
         }
-        const bool whole = lo == 0 && hi == q.units;
-        const int64_t slot = 2 * (int64_t)blockIdx.x + (lo == 0 ? 1 : 0);
-        const unsigned in_tile = row_tile * kWaveRows + (lane & 31);
-        const int64_t to = (int64_t)(q.first + (int)node) * a.Hq + qhead;
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int round = 0; round < S::kRounds; ++round) {
+            constexpr int kQuads = 16 / S::kRounds;      // of 4 dims a lane, of a round
+            if (kParts > 1) {
+                if (round) barrier();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (kParts > 1 && (t * 4 + i) / (16 / kParts) != part) continue;
-                f32x4 y = {r.o[t][4 * i], r.o[t][4 * i + 1], r.o[t][4 * i + 2], r.o[t][4 * i + 3]};
-                if (kParts > 1) {
-                    y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-                    for (int w = 0; w < kParts; ++w) {
-                        const f32x4 z = *(const __attribute__((address_space(3))) f32x4*)(
-                            shared + (((w * kRowTiles + row_tile) * 16 + t * 4 + i) * 64 + lane) * 16);
+                    for (int i = 0; i < kQuads; ++i) {
+                        const int t = (round * kQuads + i) / 4, e = (round * kQuads + i) % 4 * 4;
+                        *(lds_f32x4*)(meet + (((wave * kTiles + n) * kQuads + i) * 64 + lane) * 16) =
+                            f32x4{r.o[n][t][e], r.o[n][t][e + 1], r.o[n][t][e + 2], r.o[n][t][e + 3]};
+                    }
+                barrier();
+            }
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) y[j] = __builtin_fmaf(f[w], z[j], y[j]);
+            for (int n = 0; n < kTiles; ++n) {
+                const unsigned row = row_of(g, n), G = (unsigned)out->G, node = row / G;
+                const bool live = (int)node < g.q.nodes;
+                const int64_t to = (int64_t)(g.q.first + (int)node) * out->Hq + g.kv_head * G + row - node * G;
+                const int64_t in_slot = slot * kTileRows + row_wave * S::kWaveTile + n * kWaveRows + (lane & 31);
+                const float inv = sum[n] == 0.0f ? 0.0f : 1.0f / sum[n];
+#pragma unroll
+                for (int i = 0; i < kQuads; ++i) {
+                    if (kParts > 1 && i / (kQuads / kParts) != part) continue;
+                    const int t = (round * kQuads + i) / 4, e = (round * kQuads + i) % 4;
+                    f32x4 y = {r.o[n][t][4 * e], r.o[n][t][4 * e + 1], r.o[n][t][4 * e + 2], r.o[n][t][4 * e + 3]};
+                    if (kParts > 1) {
+                        y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int w = 0; w < kParts; ++w) {
+                            const f32x4 z = *(const lds_f32x4*)(
+                                meet + ((((w * S::kRowWaves + row_wave) * kTiles + n) * kQuads + i) * 64 + lane) * 16);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) y[j] = __builtin_fmaf(f[n][w], z[j], y[j]);
+                        }
+                    }
+                    if (!live) continue;
+                    if (whole) {
+                        y = f32x4{y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+                        *(f16x4*)(out->out + to * kRowBytes + t * 64 + e * 16 + half * 8) = __builtin_convertvector(y, f16x4);
+                    } else {
+                        *(f32x4*)(out->sums + in_slot * kHeadDim + t * 32 + e * 8 + half * 4) = y;
                     }
                 }
-                if (!live) continue;
-                if (whole) {
-                    y = f32x4{y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
-                    *(f16x4*)(a.out + to * kRowBytes + t * 64 + i * 16 + half * 8) = __builtin_convertvector(y, f16x4);
-                } else {
-                    *(f32x4*)(a.sums + (slot * kTileRows + in_tile) * kHeadDim + t * 32 + i * 8 + half * 4) = y;
+                if (round == 0 && live && part == 0 && half == 0) {
+                    if (!whole) *(f32x2*)(out->tops + in_slot * 2) = f32x2{top[n], sum[n]};
+                    else if (out->lse) out->lse[to] = (top[n] - kBias + __builtin_amdgcn_logf(sum[n])) * kLn2;
                 }
             }
         }
-        if (live && part == 0 && half == 0) {
-            if (!whole) *(f32x2*)(a.tops + (slot * kTileRows + in_tile) * 2) = f32x2{top, sum};
-            else if (a.lse) a.lse[to] = (top - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
-        }
-        if (!whole && lo == 0 && threadIdx.x == 0) {
+        if (!whole && g.lo == 0 && threadIdx.x == 0) {
             // the parts: this one and those of the next work groups up to the pair's end
-            const int64_t last = ((at + q.units) * active - 1) / total;
-            a.joins[2 * blockIdx.x] = int4{rows, (int)(last - blockIdx.x) + 1, q.first, kv_head};
-            a.joins[2 * blockIdx.x + 1] = int4{tile * kTileRows, 0, 0, 0};
+            const int to_end = g.pair_at + g.q.units - 1;         // the pair's last unit, and who takes it
+            const int owner = to_end < longer * (share + 1) ? to_end / (share + 1) : longer + (to_end - longer * (share + 1)) / share;
+            const int n_rows = min(kTileRows, g.q.nodes * out->G - g.tile * kTileRows);
+            out->joins[2 * blockIdx.x] = int4{n_rows, owner - (int)blockIdx.x + 1, g.q.first, g.kv_head};
+            out->joins[2 * blockIdx.x + 1] = int4{g.tile * kTileRows, 0, 0, 0};
         }
+        if (!more) return;
+        if (kOwn) {
+            barrier();                                   // all have met
+            load(ahead, u_ahead, 0, true);
+        }
+        if (a.negate) r.negate();
+        r.clear();
+        g = ahead;
+        u = g.lo;
+        buffer ^= 1;
     }
 }
 
@@ -360,14 +512,17 @@ __global__ __launch_bounds__(256) void join_kernel(TreeArgs a, int tile_rows)
     if (a.lse && i == 0) a.lse[to] = (top - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-int row_tiles(int max_nodes, int G)
-{
-    const int rows = max_nodes * G;
-    return rows <= kWaveRows ? 1 : rows <= 2 * kWaveRows ? 2 : 4;
-}
+// Shapes by the most rows of a pair.
+using Shape32 = Shape<1, 1, 1, 8>;
+using Shape64 = Shape<1, 2, 1, 8>;
+using Shape128 = Shape<1, 4, 2, 8>;
+using Shape256 = Shape<1, 8, 2, 8>;
 
-// Work groups that a compute unit's LDS holds.
-int groups_per_unit(int row_tiles) { return row_tiles == 1 ? 1 : 2; }
+int tile_rows(int max_nodes, int G)
+{
+    const int64_t rows = (int64_t)max_nodes * G;
+    return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+}
 
 struct Workspace {
     size_t sums, tops, joins, bytes;
@@ -405,8 +560,7 @@ size_t apex_steps_tree_workspace_bytes(int max_nodes, int Hq, int Hkv)
     if (Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 || Hq > INT_MAX / 1024 || check_nodes(max_nodes) != APEX_OK ||
         compute_units(&units) != APEX_OK)
         return 0;
-    const int waves = row_tiles(max_nodes, Hq / Hkv);
-    return lay_out(units * groups_per_unit(waves), waves * kWaveRows).bytes;
+    return lay_out(units, tile_rows(max_nodes, Hq / Hkv)).bytes;
 }
 
 int apex_steps_tree_attention(const void* q, int64_t q_token_stride, const void* k_new, const void* v_new,
@@ -460,11 +614,11 @@ int apex_steps_tree_attention(const void* q, int64_t q_token_stride, const void*
 
     if (workspace && !aligned(workspace, 256))
         return fail(APEX_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-    int units = 0;
-    rc = compute_units(&units);
+    int groups = 0;      // one on a compute unit
+    rc = compute_units(&groups);
     if (rc != APEX_OK) return rc;
-    const int waves = row_tiles(max_nodes, G), tile_rows = waves * kWaveRows, groups = units * groups_per_unit(waves);
-    const Workspace w = lay_out(groups, tile_rows);
+    const int rows = tile_rows(max_nodes, G);
+    const Workspace w = lay_out(groups, rows);
     Hold hold;
     if (workspace) {
         rc = check_workspace(workspace, workspace_bytes, w.bytes);
@@ -501,11 +655,14 @@ int apex_steps_tree_attention(const void* q, int64_t q_token_stride, const void*
     a.G = G;
     a.c = (scale < 0 ? -scale : scale) * kLog2e;
     a.negate = scale < 0;
-    const auto kernel = waves == 1 ? tree_kernel<1, 1, 8> : waves == 2 ? tree_kernel<2, 1, 4> : tree_kernel<4, 2, 4>;
-    kernel<<<groups, waves == 1 ? 512 : 256, 0, (hipStream_t)stream>>>(a);
+    const hipStream_t on = (hipStream_t)stream;
+    if (rows == 32) tree_kernel<Shape32><<<groups, 64 * Shape32::kWaves, 0, on>>>(a);
+    else if (rows == 64) tree_kernel<Shape64><<<groups, 64 * Shape64::kWaves, 0, on>>>(a);
+    else if (rows == 128) tree_kernel<Shape128><<<groups, 64 * Shape128::kWaves, 0, on>>>(a);
+    else tree_kernel<Shape256><<<groups, 64 * Shape256::kWaves, 0, on>>>(a);
     rc = launched("tree_attention");
     if (rc != APEX_OK) return rc;
-    join_kernel<<<dim3(groups, tile_rows / 8), 256, 0, (hipStream_t)stream>>>(a, tile_rows);
+    join_kernel<<<dim3(groups, rows / 8), 256, 0, on>>>(a, rows);
     return launched("tree_attention");
 }
 
