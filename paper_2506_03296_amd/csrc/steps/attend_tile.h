@@ -47,6 +47,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) f16x8 lds_f16x8;
+typedef __attribute__((address_space(3))) f16x4 lds_f16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
 
@@ -76,6 +77,15 @@ __device__ inline float sum_of_halves(float x)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// The lane, computed anew: what hangs on it does not stay in registers from one
+// use to the next.
+__device__ inline unsigned lane_again()
+{
+    unsigned x = threadIdx.x & 63;
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // A row of zeros, for rows that are not there.
 __device__ __attribute__((aligned(16))) const unsigned int kZeros[kRowBytes / 4] = {0};
 
@@ -84,13 +94,13 @@ __device__ __attribute__((aligned(16))) const unsigned int kZeros[kRowBytes / 4]
 // its loads (arrived).
 __device__ inline void load_to_lds(const char* from, unsigned to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(from) : "memory");
 }
 
 // The same from one address in all lanes and an offset of each.
 __device__ inline void load_to_lds(const char* from, unsigned offset, unsigned to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(offset), "s"(from) : "memory");
 }
 
 // Waits until all but the last n of the wave's loads have arrived and what it has
@@ -130,6 +140,14 @@ struct Rows {
             if (row) x = *(const u32x4*)(row + j * 32 + half * 16);
             q[r][j] = __builtin_bit_cast(f16x8, x);
         }
+    }
+
+    // The lane's query of tile r out of rows in LDS that lie as K's.
+    __device__ void read_q(int r, const lds_char* rows)
+    {
+        const unsigned lane = lane_again(), row = lane & 31, half = lane >> 5;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[r][j] = *(const lds_f16x8*)(rows + row * kRowBytes + k_piece(row, 2 * j + half) * 16);
     }
 
     // A negative scale is taken as its magnitude, with q's sign turned.
@@ -328,15 +346,21 @@ struct Rows {
     }
 };
 
-// The index of a call's rows: row r of a request is head r % G of its token r / G.
-struct Group {
-    int heads;       // q-heads of a kv-head (G)
-    __device__ void split(unsigned row, unsigned* token, unsigned* head) const
-    {
-        *token = row / (unsigned)heads;
-        *head = row - *token * (unsigned)heads;
-    }
+// Division by a number that the host knows, of numbers below 2^31: with s the
+// least power of two that is not below d, floor((n m / 2^32 + n) / 2^s) for
+// m = floor(2^32 (2^s - d) / d) + 1.
+struct Divisor {
+    unsigned d, m, s;
 };
+
+inline Divisor divisor(unsigned d)
+{
+    unsigned s = 0;
+    while ((1ull << s) < d) ++s;
+    return {d, (unsigned)((((1ull << s) - d) << 32) / d + 1), s};
+}
+
+__device__ inline unsigned divide(unsigned n, const Divisor& by) { return (__umulhi(n, by.m) + n) >> by.s; }
 
 // A value that is the same in all lanes, as the compiler cannot know.
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -345,32 +369,44 @@ __device__ inline int64_t uniform(int64_t x)
     return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
+template <int kControl>
+__device__ inline int moved(int x)      // within rows of 16 lanes; 0 comes in
+{
+    return __builtin_amdgcn_update_dpp(0, x, kControl, 0xf, 0xf, true);
+}
+
 // Sum over a wave's lanes.
 __device__ inline int wave_sum(int x)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
-    return uniform(x);
+    x += moved<0xb1>(x);      // lane ^ 1
+    x += moved<0x4e>(x);      // lane ^ 2
+    x += moved<0x141>(x);     // the other four of eight
+    x += moved<0x140>(x);     // the other eight of sixteen
+    return __builtin_amdgcn_readlane(x, 0) + __builtin_amdgcn_readlane(x, 16) + __builtin_amdgcn_readlane(x, 32) +
+           __builtin_amdgcn_readlane(x, 48);
 }
 
 // Largest of a wave's lanes.
 __device__ inline int wave_max(int x)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) x = max(x, __shfl_xor(x, m));
-    return uniform(x);
+    x = max(x, moved<0xb1>(x));
+    x = max(x, moved<0x4e>(x));
+    x = max(x, moved<0x141>(x));
+    x = max(x, moved<0x140>(x));
+    return max(max(__builtin_amdgcn_readlane(x, 0), __builtin_amdgcn_readlane(x, 16)),
+               max(__builtin_amdgcn_readlane(x, 32), __builtin_amdgcn_readlane(x, 48)));
 }
 
 // Inclusive sums over a wave's lanes.
 __device__ inline int wave_scan(int x)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const int y = __shfl_up(x, m);
-        if (lane >= m) x += y;
-    }
-    return x;
+    x += moved<0x111>(x);     // from 1, 2, 4 and 8 lanes below
+    x += moved<0x112>(x);
+    x += moved<0x114>(x);
+    x += moved<0x118>(x);
+    const int a = __builtin_amdgcn_readlane(x, 15), b = a + __builtin_amdgcn_readlane(x, 31);
+    const int c = b + __builtin_amdgcn_readlane(x, 47), row = (threadIdx.x & 63) >> 4;
+    return x + (row == 0 ? 0 : row == 1 ? a : row == 2 ? b : c);
 }
 
 }  // namespace steps

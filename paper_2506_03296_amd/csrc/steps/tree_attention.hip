@@ -198,7 +198,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
     const auto load = [&](const Segment& g, int u, int buffer, bool is_v) {
         const Arguments f = arguments();
         const char* const head = (is_v ? f->v_cache : f->k_cache) + (int64_t)g.kv_head * kSlabBytes;
-        const unsigned to = (unsigned)uniform((int)(lds_address(shared) + buffer * 2 * kBytes + (is_v ? kBytes : 0)));
+        const unsigned to = lds_address(shared) + buffer * 2 * kBytes + (is_v ? kBytes : 0);
         const unsigned quad = lane >> 4;                 // the lane's key of a load's four
         const int left = u < g.cached ? g.q.len - u * kKeys : g.q.nodes;
         bool plain = first_key(kLoads - 1) + 4 <= left;
