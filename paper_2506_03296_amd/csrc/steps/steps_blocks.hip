@@ -160,16 +160,22 @@ constexpr int kReleaseThreads = 1024;
 constexpr int kEntries = 8;      // of a thread at a time
 
 // One work group: where an id goes depends on how many of those before it count.
+// It takes 8192 entries of the rows at a time, neighbouring lanes neighbouring
+// entries, and ranks them by the waves' votes.
 __global__ __launch_bounds__(kReleaseThreads) void release_kernel(ReleaseArgs a)
 {
-    constexpr int kThreads = kReleaseThreads;
-    __shared__ int64_t part[kThreads / 64];
+    constexpr int kThreads = kReleaseThreads, kWaves = kThreads / 64, kVotes = kEntries * kWaves;
+    static_assert(kVotes == 128, "two votes a lane");
+    __shared__ int64_t part[kWaves];
     __shared__ int64_t upto[kThreads];
     __shared__ int32_t firsts[kThreads];
+    __shared__ int votes[2][kVotes];
+    const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
     int64_t height = min((int64_t)max(a.state[0], 0), a.num_blocks);
     const unsigned bs = (unsigned)a.block_size;
+    unsigned turn = 0;
     for (int base = 0; base < a.B; base += kThreads) {
-        const int b = base + (int)threadIdx.x, n_here = min(kThreads, a.B - base);
+        const int b = base + (int)threadIdx.x;
         int64_t first = 0, n = 0;
         if (b < a.B) {
             first = ((unsigned)max(a.keeps[b], 0) + bs - 1) / bs;
@@ -180,35 +186,46 @@ __global__ __launch_bounds__(kReleaseThreads) void release_kernel(ReleaseArgs a)
         upto[threadIdx.x] = group_scan<kThreads>(n, part, &all);
         firsts[threadIdx.x] = (int32_t)first;
         __syncthreads();
-        for (int64_t i0 = 0; i0 < all; i0 += kThreads * kEntries) {
-            const int64_t i = i0 + (int64_t)threadIdx.x * kEntries;
+        const int64_t coarse = upto[16 * lane + 15];
+        for (int64_t i0 = 0; i0 < all; i0 += kThreads * kEntries, turn ^= 1) {
+            int32_t* at[kEntries];
             int32_t id[kEntries];
-            int64_t count = 0;
-            int r = i < all ? find(upto, n_here, i) : 0;
-            int64_t at[kEntries];
 #pragma unroll
             for (int e = 0; e < kEntries; ++e) {
-                at[e] = -1;
+                // the row of the wave's first entry, among the work group's 1024 in two
+                // steps, and from there on the lane's own
+                const int64_t i_wave = i0 + e * kThreads + wave * 64, i = i_wave + lane;
+                at[e] = nullptr;
                 id[e] = -1;
-                if (i + e >= all) continue;
-                while (upto[r] <= i + e) ++r;
-                at[e] = (base + r) * a.table_stride + firsts[r] + (i + e - (r ? upto[r - 1] : 0));
-                id[e] = a.table[at[e]];
-            }
-#pragma unroll
-            for (int e = 0; e < kEntries; ++e)
-                if (id[e] >= 0 && id[e] < a.num_blocks) ++count;
-            int64_t pushed;
-            int64_t to = height + group_scan<kThreads>(count, part, &pushed) - count;
-#pragma unroll
-            for (int e = 0; e < kEntries; ++e) {
-                if (at[e] >= 0) a.table[at[e]] = -1;
-                if (id[e] >= 0 && id[e] < a.num_blocks) {
-                    if (to < a.num_blocks) a.free_blocks[to] = id[e];
-                    ++to;
+                if (i_wave >= all) continue;
+                const int sixteen = 16 * __builtin_popcountll(__ballot(coarse <= i_wave));
+                int r = sixteen + __builtin_popcountll(__ballot(lane < 16 && upto[min(sixteen + lane, kThreads - 1)] <= i_wave));
+                if (i < all) {
+                    for (int step = 0; step < 4 && upto[r] <= i; ++step) ++r;
+                    if (upto[r] <= i) r += find(upto + r, kThreads - r, i);      // many rows with little or nothing to give
+                    at[e] = a.table + (base + r) * a.table_stride + firsts[r] + (i - (r ? upto[r - 1] : 0));
+                    id[e] = *at[e];
                 }
             }
-            height = min(height + pushed, a.num_blocks);
+            uint64_t counts[kEntries];
+#pragma unroll
+            for (int e = 0; e < kEntries; ++e) {
+                counts[e] = __ballot(id[e] >= 0 && id[e] < a.num_blocks);
+                if (lane == 0) votes[turn][e * kWaves + wave] = __builtin_popcountll(counts[e]);
+            }
+            __syncthreads();
+            // votes before each of this wave's, two of all to a lane
+            const int v0 = votes[turn][2 * lane], v1 = votes[turn][2 * lane + 1];
+            const int sum = wave_scan(v0 + v1), before = sum - v0 - v1;
+#pragma unroll
+            for (int e = 0; e < kEntries; ++e) {
+                const int vote = e * kWaves + wave;
+                const int ahead = __builtin_amdgcn_readlane(before, vote / 2) + (vote & 1 ? __builtin_amdgcn_readlane(v0, vote / 2) : 0);
+                const int64_t to = height + ahead + __builtin_popcountll(counts[e] & ((1ull << lane) - 1));
+                if (at[e]) *at[e] = -1;
+                if ((counts[e] >> lane & 1) && to < a.num_blocks) a.free_blocks[to] = id[e];
+            }
+            height = min(height + __builtin_amdgcn_readlane(sum, 63), a.num_blocks);
         }
         __syncthreads();
     }

@@ -172,11 +172,9 @@ def new_pool(num_blocks, device):
 def empty_plan(B, T, device):
     """An uninitialised plan for ``extend`` to write."""
     torch = _torch()
-    # one piece of memory: the 64-bit array first, the others behind it
-    T8 = T * 8
-    mem = torch.empty(T8 + 4 * (B + 1 + B + T), dtype=torch.uint8, device=device)
-    words = mem[T8:].view(torch.int32)
-    return Plan(words[:B + 1], words[B + 1:2 * B + 1], mem[:T8].view(torch.int64), words[2 * B + 1:])
+    i32 = torch.int32
+    return Plan(torch.empty(B + 1, dtype=i32, device=device), torch.empty(B, dtype=i32, device=device),
+                torch.empty(T, dtype=torch.int64, device=device), torch.empty(T, dtype=i32, device=device))
 
 
 def extend(context_lens, new_lens, block_table, free_blocks, free_state, T, block_size=BLOCK_SIZE, plan=None,
