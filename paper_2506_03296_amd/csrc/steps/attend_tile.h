@@ -97,10 +97,12 @@ __device__ inline void load_to_lds(const char* from, unsigned to)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(from) : "memory");
 }
 
-// The same from one address in all lanes and an offset of each.
-__device__ inline void load_to_lds(const char* from, unsigned offset, unsigned to)
+// The same from one address in all lanes and an offset of each, past the caches:
+// what is read once (a batch of 32 long contexts: 282 us, 315 by way of them).
+__device__ inline void stream_to_lds(const char* from, unsigned offset, unsigned to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(offset), "s"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(__builtin_amdgcn_readfirstlane((int)to)),
+                 "v"(offset), "s"(from) : "memory");
 }
 
 // Waits until all but the last n of the wave's loads have arrived and what it has
@@ -360,7 +362,8 @@ inline Divisor divisor(unsigned d)
     return {d, (unsigned)((((1ull << s) - d) << 32) / d + 1), s};
 }
 
-__device__ inline unsigned divide(unsigned n, const Divisor& by) { return (__umulhi(n, by.m) + n) >> by.s; }
+template <class D>
+__device__ inline unsigned divide(unsigned n, const D& by) { return (__umulhi(n, by.m) + n) >> by.s; }
 
 // A value that is the same in all lanes, as the compiler cannot know.
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }

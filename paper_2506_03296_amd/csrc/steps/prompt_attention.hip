@@ -306,7 +306,10 @@ extern "C" int apex_steps_prompt_attention(const void* q, int64_t q_token_stride
     a.G = divisor((unsigned)(Hq / Hkv));
     a.c = (scale < 0 ? -scale : scale) * kLog2e;
     a.negate = scale < 0;
-    constexpr int kWaves = 8, kRows = kWaves * kWaveRows;
+#ifndef PW
+#define PW 8
+#endif
+    constexpr int kWaves = PW, kRows = kWaves * kWaveRows;
     const unsigned slots = (unsigned)((int64_t)T * a.G.d / kRows) + (unsigned)B;
     int units = 0;
     rc = compute_units(&units);

@@ -14,7 +14,7 @@ constexpr int kSlabBytes = kBlockSize * kRowBytes;
 // All pairs' units lie in one row, each pair's behind kPairCost units that stand for
 // its start; the work groups that take part get equal shares of it.
 constexpr int kPairCost = 1;
-constexpr int kLeastShare = 2;
+constexpr int kLeastShare = 1;
 
 struct TreeArgs {
     const char *q, *k_new, *v_new, *k_cache, *v_cache;
@@ -27,7 +27,8 @@ struct TreeArgs {
     int4* joins;                   // [groups] the pair that the group's last part opens
     int64_t q_stride, new_stride;  // bytes between tokens
     int64_t table_stride, num_blocks;
-    int B, T, max_nodes, Hq, Hkv, G;
+    int B, T, max_nodes, Hq, Hkv;
+    Divisor G;
     float c;
     bool negate;
 };
@@ -56,7 +57,7 @@ __device__ inline Request read_request(const Args& a, int b)
     r.nodes = min(hi - lo, a.max_nodes);
     r.len = (int)min((int64_t)max(a.lens[b], 0), a.table_stride * kBlockSize);
     r.units = r.nodes ? (int)(((int64_t)r.len + kKeys - 1) / kKeys) + 1 : 0;
-    r.tiles = (r.nodes * a.G + kTileRows - 1) / kTileRows;
+    r.tiles = (r.nodes * (int)a.G.d + kTileRows - 1) / kTileRows;
     return r;
 }
 
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
                 const unsigned in_block = kOwn ? (j & 3) * 4 : (wave & 3) * 4;
                 const unsigned offset = (in_block + quad) * kRowBytes
                                         + (is_v ? v_piece(quad, lane & 15) : k_piece(in_block + quad, lane & 15)) * 16;
-                load_to_lds(head + (int64_t)ids[kOwn ? j / 4 : j] * block_bytes, offset, to + first_key(j) * kRowBytes);
+                stream_to_lds(head + (int64_t)ids[kOwn ? j / 4 : j] * block_bytes, offset, to + first_key(j) * kRowBytes);
             }
             return;
         }
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
         const Arguments f = arguments();
 #pragma unroll
         for (int i = 0; i < kTiles; ++i) {
-            const unsigned row = row_of(g, i), G = (unsigned)f->G, node = row / G;
+            const unsigned row = row_of(g, i), G = f->G.d, node = divide(row, f->G);
             const bool live = (int)node < g.q.nodes;
             r.start(i, live ? f->q + (int64_t)(g.q.first + (int)node) * f->q_stride + (g.kv_head * G + row - node * G) * kRowBytes
                             : nullptr);
@@ -427,7 +428,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
             }
 #pragma unroll
             for (int n = 0; n < kTiles; ++n) {
-                const unsigned row = row_of(g, n), G = (unsigned)out->G, node = row / G;
+                const unsigned row = row_of(g, n), G = out->G.d, node = divide(row, out->G);
                 const bool live = (int)node < g.q.nodes;
                 const int64_t to = (int64_t)(g.q.first + (int)node) * out->Hq + g.kv_head * G + row - node * G;
                 const int64_t in_slot = slot * kTileRows + row_wave * S::kWaveTile + n * kWaveRows + (lane & 31);
@@ -465,7 +466,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
             // the parts: this one and those of the next work groups up to the pair's end
             const int to_end = g.pair_at + g.q.units - 1;         // the pair's last unit, and who takes it
             const int owner = to_end < longer * (share + 1) ? to_end / (share + 1) : longer + (to_end - longer * (share + 1)) / share;
-            const int n_rows = min(kTileRows, g.q.nodes * out->G - g.tile * kTileRows);
+            const int n_rows = min(kTileRows, g.q.nodes * (int)out->G.d - g.tile * kTileRows);
             out->joins[2 * blockIdx.x] = int4{n_rows, owner - (int)blockIdx.x + 1, g.q.first, g.kv_head};
             out->joins[2 * blockIdx.x + 1] = int4{g.tile * kTileRows, 0, 0, 0};
         }
@@ -505,8 +506,8 @@ __global__ __launch_bounds__(256) void join_kernel(TreeArgs a, int tile_rows)
         top = to;
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const int node = at / a.G;
-    const int64_t to = (int64_t)(job.z + node) * a.Hq + job.w * a.G + (at - node * a.G);
+    const int G = (int)a.G.d, node = (int)divide((unsigned)at, a.G);
+    const int64_t to = (int64_t)(job.z + node) * a.Hq + job.w * G + (at - node * G);
     y = f32x4{y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
     *(f16x4*)(a.out + to * kRowBytes + i * 8) = __builtin_convertvector(y, f16x4);
     if (a.lse && i == 0) a.lse[to] = (top - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
@@ -652,7 +653,7 @@ int apex_steps_tree_attention(const void* q, int64_t q_token_stride, const void*
     a.max_nodes = max_nodes;
     a.Hq = Hq;
     a.Hkv = Hkv;
-    a.G = G;
+    a.G = divisor((unsigned)G);
     a.c = (scale < 0 ? -scale : scale) * kLog2e;
     a.negate = scale < 0;
     const hipStream_t on = (hipStream_t)stream;

@@ -20,12 +20,11 @@ result that the call allocates belongs to the stream it works on: to use it on
 another one, wait for the call there, and record_stream before it is dropped, as
 with any tensor of torch's.
 """
-import contextlib
 import ctypes
 import os
 from typing import NamedTuple
 
-from . import APEX_ERR_HIP, APEX_OK, ApexError, _on, _raw_stream, _require, _torch
+from . import APEX_ERR_HIP, APEX_OK, ApexError, _on, _raw_stream, _require, _result, _torch
 
 __all__ = ["LIB_PATH", "EXPORTED_SYMBOLS", "BLOCK_SIZE", "HEAD_DIM", "MAX_NODES", "Plan", "load_library", "last_error",
            "new_pool", "empty_plan", "extend", "release", "prompt_attention", "tree_attention", "tree_workspace_bytes",
@@ -129,11 +128,6 @@ def _gpu(t, name):
     return t.device, t.get_device()
 
 
-def _allocate(stream):
-    """Where a call's results are made: on the stream that writes them."""
-    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
-
-
 def _table(block_table, B, device, index):
     """Entries per row."""
     if block_table.dim() != 2 or block_table.shape[0] != B:
@@ -196,8 +190,11 @@ def extend(context_lens, new_lens, block_table, free_blocks, free_state, T, bloc
     if plan is None:
         if T < 0:
             raise ValueError(f"T = {T} is negative")
-        with _allocate(stream):
+        if stream is None:
             plan = empty_plan(B, T, dev)
+        else:
+            with torch.cuda.stream(stream):
+                plan = empty_plan(B, T, dev)
     else:
         _want(plan.token_offsets, "token_offsets", i32, (B + 1,), dev, index)
         _want(plan.total_lens, "total_lens", i32, (B,), dev, index)
@@ -227,9 +224,34 @@ def release(context_lens, keep_lens, block_table, free_blocks, free_state, block
           free_blocks.data_ptr(), free_state.data_ptr(), B, block_size, nb, _raw_stream(stream, index))
 
 
-def _packed(q, k, v, names, token_offsets, out, lse_out, stream):
-    """Checks common to the attentions: (device, index, B, T, Hq, Hkv, strides, out)."""
+# The checks of tensors cost 4 us of Python where a small batch's kernel takes 6.
+# _plain answers the common case -- everything as it must be -- with a few attribute
+# reads; anything else goes through the checks, which raise what they find.
+
+def _plain(q, k, v, token_offsets):
+    """(index, B, T, Hq, Hkv, q's and k's elements between tokens) if the checks
+    accept the tensors for sure, else None."""
     torch = _torch()
+    f16 = torch.float16
+    qs, ks, os_ = q.shape, k.shape, token_offsets.shape
+    if (len(qs) == 3 and len(ks) == 3 and len(os_) == 1 and os_[0] > 0 and v.shape == ks and qs[0] == ks[0] > 1
+            and qs[2] == HEAD_DIM and ks[2] == HEAD_DIM and q.is_cuda and q.dtype is f16 and k.dtype is f16
+            and v.dtype is f16 and token_offsets.dtype is torch.int32):
+        i = q.get_device()
+        if k.get_device() == i and v.get_device() == i and token_offsets.get_device() == i:
+            q0, q1, q2 = q.stride()
+            kt = k.stride()
+            if (v.stride() == kt and q1 == HEAD_DIM and kt[1] == HEAD_DIM and q2 == 1 and kt[2] == 1
+                    and q0 >= qs[1] * HEAD_DIM and kt[0] >= ks[1] * HEAD_DIM and token_offsets.is_contiguous()):
+                return i, os_[0] - 1, qs[0], qs[1], ks[1], q0, kt[0]
+    return None
+
+
+def _packed(q, k, v, names, token_offsets):
+    """As _plain, with an error for what is not so."""
+    plain = _plain(q, k, v, token_offsets)
+    if plain is not None:
+        return plain
     dev, index = _gpu(q, "q")
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError(f"q, {names[0]} and {names[1]} must be [T][heads][{HEAD_DIM}]")
@@ -243,15 +265,24 @@ def _packed(q, k, v, names, token_offsets, out, lse_out, stream):
     B = token_offsets.numel() - 1
     if B < 0:
         raise ValueError("token_offsets must be [B + 1]")
-    _want(token_offsets, "token_offsets", torch.int32, (B + 1,), dev, index)
+    _want(token_offsets, "token_offsets", _torch().int32, (B + 1,), dev, index)
+    return index, B, T, Hq, Hkv, q_stride, k_stride
+
+
+def _outputs(q, T, Hq, index, out, lse_out, stream):
+    """(out, address of lse_out)."""
+    torch = _torch()
     if out is None:
-        with _allocate(stream):
-            out = torch.empty((T, Hq, HEAD_DIM), dtype=torch.float16, device=dev)
+        if stream is None:
+            out = torch.empty((T, Hq, HEAD_DIM), dtype=torch.float16, device=q.device)
+        else:
+            out = _result((T, Hq, HEAD_DIM), q.device, stream)
     else:
-        _want(out, "out", torch.float16, (T, Hq, HEAD_DIM), dev, index)
-    if lse_out is not None:
-        _want(lse_out, "lse_out", torch.float32, (T, Hq), dev, index)
-    return dev, index, B, T, Hq, Hkv, q_stride, k_stride, out
+        _want(out, "out", torch.float16, (T, Hq, HEAD_DIM), q.device, index)
+    if lse_out is None:
+        return out, None
+    _want(lse_out, "lse_out", torch.float32, (T, Hq), q.device, index)
+    return out, lse_out.data_ptr()
 
 
 def prompt_attention(q, k, v, token_offsets, scale, out=None, lse_out=None, stream=None):
@@ -261,10 +292,10 @@ def prompt_attention(q, k, v, token_offsets, scale, out=None, lse_out=None, stre
     q [T][Hq][128], k and v [T][Hkv][128] (fp16) with unit strides inside a token;
     the token strides may be wider (views into a fused QKV buffer), k's and v's the
     same.  Rows behind token_offsets[-1] are left as they are."""
-    _, index, B, T, Hq, Hkv, qs, ks, out = _packed(q, k, v, ("k", "v"), token_offsets, out, lse_out, stream)
+    index, B, T, Hq, Hkv, qs, ks = _packed(q, k, v, ("k", "v"), token_offsets)
+    out, lse = _outputs(q, T, Hq, index, out, lse_out, stream)
     _call("apex_steps_prompt_attention", index, q.data_ptr(), qs, k.data_ptr(), v.data_ptr(), ks,
-          token_offsets.data_ptr(), out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), B, T, Hq, Hkv,
-          HEAD_DIM, scale, _raw_stream(stream, index))
+          token_offsets.data_ptr(), out.data_ptr(), lse, B, T, Hq, Hkv, HEAD_DIM, scale, _raw_stream(stream, index))
     return out
 
 
@@ -278,8 +309,8 @@ def tree_attention(q, k_new, v_new, token_offsets, tree_mask, k_cache, v_cache, 
     is an optional uint8 tensor of tree_workspace_bytes(max_nodes, Hq, Hkv) bytes;
     calls that can overlap, and a captured graph, need one of their own."""
     torch = _torch()
-    dev, index, B, T, Hq, Hkv, qs, ks, out = _packed(q, k_new, v_new, ("k_new", "v_new"), token_offsets, out, lse_out,
-                                                     stream)
+    index, B, T, Hq, Hkv, qs, ks = _packed(q, k_new, v_new, ("k_new", "v_new"), token_offsets)
+    dev = q.device
     _want(tree_mask, "tree_mask", torch.int64, (T,), dev, index)
     shape = k_cache.shape
     if len(shape) != 4 or shape[1] != Hkv or shape[2] != BLOCK_SIZE or shape[3] != HEAD_DIM:
@@ -293,8 +324,8 @@ def tree_attention(q, k_new, v_new, token_offsets, tree_mask, k_cache, v_cache, 
         if not (_on(workspace, torch.uint8, index) and workspace.is_contiguous()):
             _require(workspace, "workspace", torch.uint8, dev)
         ws, ws_bytes = workspace.data_ptr(), workspace.numel()
+    out, lse = _outputs(q, T, Hq, index, out, lse_out, stream)
     _call("apex_steps_tree_attention", index, q.data_ptr(), qs, k_new.data_ptr(), v_new.data_ptr(), ks,
           token_offsets.data_ptr(), tree_mask.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(),
-          stride, context_lens.data_ptr(), out.data_ptr(), None if lse_out is None else lse_out.data_ptr(), B, T,
-          max_nodes, Hq, Hkv, HEAD_DIM, BLOCK_SIZE, shape[0], scale, ws, ws_bytes, _raw_stream(stream, index))
+          stride, context_lens.data_ptr(), out.data_ptr(), lse, B, T, max_nodes, Hq, Hkv, HEAD_DIM, BLOCK_SIZE, shape[0], scale, ws, ws_bytes, _raw_stream(stream, index))
     return out
