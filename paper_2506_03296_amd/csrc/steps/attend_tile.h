@@ -214,36 +214,38 @@ struct Rows {
         }
     }
 
-    // Weights of tile r's scores, as P^T's operands: keys 16 w + 4 half + 0..3 and + 8 in p[w].
-    __device__ void weights(int r, const f32x16 (&s)[kSub], float c, f16x8 (&p)[2 * kSub])
+    // The running maximum of tile r after these scores.
+    __device__ void raise(int r, const f32x16 (&s)[kSub], float c)
     {
-        float m = -INFINITY;
+        float m[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};      // four chains
 #pragma unroll
         for (int u = 0; u < kSub; ++u)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) m = fmaxf(m, s[u][i]);
-        m = max_of_halves(m) * c;
-        if (__builtin_expect(__any(m > top[r] + kSlack), 0)) rescale(r, fmaxf(m, top[r]));
+            for (int i = u ? 0 : 4; i < 16; ++i) m[i & 3] = fmaxf(m[i & 3], s[u][i]);
+        const float most = max_of_halves(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))) * c;
+        if (__builtin_expect(__any(most > top[r] + kSlack), 0)) rescale(r, fmaxf(most, top[r]));
+    }
+
+    // Weights of 32 keys' scores of tile r, as P^T's operands: keys 16 w + 4 half + 0..3 and + 8 in p[w].
+    __device__ void weights(int r, const f32x16& s, float c, f16x8* p)
+    {
         // a row that has seen no score yet keeps M = -inf: 2^(-inf - 0) = 0
         const float base = (top[r] == -INFINITY ? 0.0f : top[r]) - kBias;
-        float part = 0.0f;
+        float part[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int u = 0; u < kSub; ++u)
+        for (int w = 0; w < 2; ++w)
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
-#pragma unroll
-                for (int j = 0; j < 8; j += 2) {
-                    f32x2 e;
-                    e[0] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][8 * w + j], c, -base));
-                    e[1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][8 * w + j + 1], c, -base));
-                    part += e[0];
-                    part += e[1];
-                    const f16x2 h = __builtin_convertvector(e, f16x2);
-                    p[2 * u + w][j] = h[0];
-                    p[2 * u + w][j + 1] = h[1];
-                }
+            for (int j = 0; j < 8; j += 2) {
+                f32x2 e;
+                e[0] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * w + j], c, -base));
+                e[1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * w + j + 1], c, -base));
+                part[0] += e[0];
+                part[1] += e[1];
+                const f16x2 h = __builtin_convertvector(e, f16x2);
+                p[w][j] = h[0];
+                p[w][j + 1] = h[1];
             }
-        sum[r] += part;
+        sum[r] += part[0] + part[1];
     }
 
     __device__ void rescale(int r, float to)
@@ -268,36 +270,43 @@ struct Rows {
         return __builtin_bit_cast(f16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
     }
 
-    // The operands of `n` steps from step w on.
-    template <int n>
-    __device__ static void read_v(const lds_char* v, int w, f16x8 (&a)[n][4])
+    // The operands of 32 keys, two steps.
+    __device__ static void read_v(const lds_char* v, int u, f16x8 (&a)[2][4])
     {
 #pragma unroll
-        for (int i = 0; i < n; ++i)
+        for (int w = 0; w < 2; ++w)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) a[i][t] = v_operand(v, w + i, t);
+            for (int t = 0; t < 4; ++t) a[w][t] = v_operand(v, 2 * u + w, t);
         __builtin_amdgcn_sched_barrier(0);
     }
 
-    template <int n>
-    __device__ void add(int w, const f16x8 (&a)[n][4], const f16x8 (&p)[kTiles][2 * kSub])
+    __device__ void add(int r, const f16x8 (&a)[2][4], const f16x8* p)
     {
 #pragma unroll
-        for (int i = 0; i < n; ++i)
+        for (int w = 0; w < 2; ++w)
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int r = 0; r < kTiles; ++r)
-                    o[r][t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][t], p[r][w + i], o[r][t], 0, 0, 0);
+            for (int t = 0; t < 4; ++t) o[r][t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[w][t], p[w], o[r][t], 0, 0, 0);
     }
 
-    __device__ void add(const lds_char* v, const f16x8 (&p)[kTiles][2 * kSub])
+    // The weights of a unit's scores and their products with V: V's operands come
+    // while weights are made, and the weights of 32 keys are made while the matrix
+    // cores work on the 32 before them.
+    __device__ void take(const f32x16 (&s)[kTiles][kSub], float c, const lds_char* v)
     {
 #pragma unroll
-        for (int w = 0; w < 2 * kSub; w += 2) {
+        for (int u = 0; u < kSub; ++u) {
             f16x8 a[2][4];
-            read_v(v, w, a);
-            add(w, a, p);
+            read_v(v, u, a);
+            if (u == 0) {
+#pragma unroll
+                for (int r = 0; r < kTiles; ++r) raise(r, s[r], c);
+            }
+#pragma unroll
+            for (int r = 0; r < kTiles; ++r) {
+                f16x8 p[2];
+                weights(r, s[r][u], c, p);
+                add(r, a, p);
+            }
         }
     }
 

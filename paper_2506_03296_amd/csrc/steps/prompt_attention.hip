@@ -210,14 +210,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
             bring(t);
             const lds_char* kt = shared + buffer * 2 * kTileBytes;
             f32x16 s[1][2];
-            f16x8 p[1][4];
             r.scores(kt, s);
             if ((t + 1) * kKeys > wave_lo + 1) {
                 const int seen = pos - t * kKeys + 1;       // keys of the tile up to the row's own
                 r.mask(s[0], seen >= 64 ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
             }
-            r.weights(0, s[0], a.c, p[0]);
-            r.add(kt + kTileBytes, p);
+            r.take(s, a.c, kt + kTileBytes);
             buffer ^= 1;
             if (t + 1 < tiles) {
                 arrived<0>();
@@ -306,10 +304,7 @@ extern "C" int apex_steps_prompt_attention(const void* q, int64_t q_token_stride
     a.G = divisor((unsigned)(Hq / Hkv));
     a.c = (scale < 0 ? -scale : scale) * kLog2e;
     a.negate = scale < 0;
-#ifndef PW
-#define PW 8
-#endif
-    constexpr int kWaves = PW, kRows = kWaves * kWaveRows;
+    constexpr int kWaves = 8, kRows = kWaves * kWaveRows;
     const unsigned slots = (unsigned)((int64_t)T * a.G.d / kRows) + (unsigned)B;
     int units = 0;
     rc = compute_units(&units);

@@ -293,7 +293,6 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
         }
         lds_char* const kt = shared + (kOwn ? 0 : buffer * 2 * kBytes) + from * kRowBytes;
         f32x16 s[kTiles][kSub];
-        f16x8 p[kTiles][2 * kSub];
         r.scores(kt, s);
         if (kOwn && more) {
             was_read();
@@ -316,26 +315,13 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
             for (int i = 0; i < kTiles; ++i) r.mask(s[i], tree[i] >> (from & 63) & nodes);
         }
         if (kOwn) {
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i) r.weights(i, s[i], c, p[i]);
             if (more) arrived<kLoads>();                 // V; the next K is on its way
             else arrived<0>();
-            r.add(kt + kBytes, p);
-            if (!last) {
-                was_read();
-                load(ahead, u_ahead, 0, true);
-            }
-        } else {
-            // V's operands come while the weights are made
-            f16x8 v[2][4];
-            r.read_v(kt + kBytes, 0, v);
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i) r.weights(i, s[i], c, p[i]);
-            r.add(0, v, p);
-            if (kSub == 2) {
-                r.read_v(kt + kBytes, 2, v);
-                r.add(2, v, p);
-            }
+        }
+        r.take(s, c, kt + kBytes);
+        if (kOwn && !last) {
+            was_read();
+            load(ahead, u_ahead, 0, true);
         }
         there = present();
         if (!last) {
