@@ -200,7 +200,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
         const Arguments f = arguments();
         const char* const head = (is_v ? f->v_cache : f->k_cache) + (int64_t)g.kv_head * kSlabBytes;
         const unsigned to = lds_address(shared) + buffer * 2 * kBytes + (is_v ? kBytes : 0);
-        const unsigned quad = lane >> 4;                 // the lane's key of a load's four
+        const unsigned lane = lane_again(), quad = lane >> 4;      // the lane's key of a load's four
         const int left = u < g.cached ? g.q.len - u * kKeys : g.q.nodes;
         bool plain = first_key(kLoads - 1) + 4 <= left;
 #pragma unroll
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
     Rows<kSub, kTiles> r;
     uint64_t tree[kTiles];                               // the drafted tokens that the lane's rows see
     const auto row_of = [&](const Segment& g, int i) {
-        return (unsigned)(g.tile * kTileRows + row_wave * S::kWaveTile + i * kWaveRows) + (lane & 31);
+        return (unsigned)(g.tile * kTileRows + row_wave * S::kWaveTile + i * kWaveRows) + (lane_again() & 31);
     };
     const auto rows = [&](const Segment& g, uint64_t (&words)[kTiles]) {
         const Arguments f = arguments();
@@ -479,6 +479,7 @@ __global__ __launch_bounds__(256) void join_kernel(TreeArgs a, int tile_rows)
     const int at = a.joins[2 * blockIdx.x + 1].x + row;
     float top = -INFINITY, sum = 0.0f;
     f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
     for (int p = 0; p < job.y; ++p) {
         const int64_t slot = p == 0 ? 2 * (int64_t)blockIdx.x + 1 : 2 * ((int64_t)blockIdx.x + p);
         const f32x2 ts = *(const f32x2*)(a.tops + (slot * tile_rows + row) * 2);
