@@ -31,8 +31,8 @@
  * Scores, softmax and sums are fp32, the softmax's weights enter the product
  * with V as fp16.  A row that attends nothing gives zeros and -inf.  What a row
  * does not attend has no influence on it, infinities and NaNs among it.
- * Supported: d = 128, B <= 2^22, (T + 256) * Hq < 2^30, strides < 2^31; block_size
- * 16 for the attention, any for extend and release; anything else returns
+ * Supported: d = 128, B <= 2^22, Hq <= 2^16, (T + 256) * Hq < 2^30, B * Hkv + (T + 32) *
+ * Hq / 32 < 2^30, strides < 2^31; block_size 16 for the attention, any for extend and release; anything else returns
  * APEX_ERR_UNSUPPORTED.
  *
  * Ownership and errors as in apex_decode.h: the caller owns every buffer, a

@@ -58,7 +58,7 @@ int check_attention(int B, int T, int Hq, int Hkv, int d, float scale, int64_t* 
     if (Hq <= 0 || Hq % Hkv != 0)
         return fail(APEX_ERR_INVALID_ARG, "Hq = %d must be a positive multiple of Hkv = %d", Hq, Hkv);
     if (d != 128) return fail(APEX_ERR_UNSUPPORTED, "head dim %d unsupported (only 128)", d);
-    if (Hq > INT_MAX / 1024) return fail(APEX_ERR_UNSUPPORTED, "Hq = %d unsupported", Hq);
+    if (Hq > kMostHeads) return fail(APEX_ERR_UNSUPPORTED, "Hq = %d exceeds %d", Hq, kMostHeads);
     if (((int64_t)T + 256) * Hq > INT_MAX / 2) return fail(APEX_ERR_UNSUPPORTED, "(T + 256) * Hq reaches 2^30");
     if (B > (1 << 22)) return fail(APEX_ERR_UNSUPPORTED, "B exceeds 2^22");
     if (((int64_t)B + (int64_t)(T / 32 + 1) * (Hq / Hkv)) * Hkv > INT_MAX / 2)

@@ -15,6 +15,9 @@ namespace steps __attribute__((visibility("hidden"))) {
 
 using apex::fail;
 
+// Bytes of a block of 16 tokens' K of all kv-heads stay far below 2^32.
+constexpr int kMostHeads = 1 << 16;
+
 inline bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }

@@ -545,7 +545,7 @@ size_t apex_steps_tree_workspace_bytes(int max_nodes, int Hq, int Hkv)
     using namespace steps;
     apex::clear_error();
     int units = 0;
-    if (Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 || Hq > INT_MAX / 1024 || check_nodes(max_nodes) != APEX_OK ||
+    if (Hkv <= 0 || Hq <= 0 || Hq % Hkv != 0 || Hq > kMostHeads || check_nodes(max_nodes) != APEX_OK ||
         compute_units(&units) != APEX_OK)
         return 0;
     return lay_out(units, tile_rows(max_nodes, Hq / Hkv)).bytes;

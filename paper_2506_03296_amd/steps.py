@@ -121,6 +121,15 @@ def _want(t, name, dtype, shape, device, index):
         _require(t, name, dtype, device, shape=shape)
 
 
+def _words(tensors, shapes, index):
+    """True if all are contiguous int32 tensors of these shapes on GPU `index`."""
+    i32 = _torch().int32
+    for t, shape in zip(tensors, shapes):
+        if not (t.dtype is i32 and t.shape == shape and t.get_device() == index and t.is_contiguous()):
+            return False
+    return True
+
+
 def _gpu(t, name):
     """(device, index) of a tensor that has to be on a GPU."""
     if not t.is_cuda:
@@ -155,6 +164,21 @@ def _rows(t, name, heads, device, index):
     return s[0]
 
 
+def _blocks(context_lens, lens, name, block_table, free_blocks, free_state):
+    """Checks common to extend and release: (device, index, B, entries per table row, blocks)."""
+    dev, index = _gpu(block_table, "block_table")
+    B, nb, shape = context_lens.numel(), free_blocks.numel(), block_table.shape
+    if not (len(shape) == 2 and shape[0] == B
+            and _words((block_table, context_lens, lens, free_blocks, free_state), (shape, (B,), (B,), (nb,), (2,)), index)):
+        i32 = _torch().int32
+        _want(context_lens, "context_lens", i32, (B,), dev, index)
+        _want(lens, name, i32, (B,), dev, index)
+        _table(block_table, B, dev, index)
+        _want(free_blocks, "free_blocks", i32, (nb,), dev, index)
+        _want(free_state, "free_state", i32, (2,), dev, index)
+    return dev, index, B, shape[1], nb
+
+
 def new_pool(num_blocks, device):
     """(free_blocks, free_state) of a cache whose num_blocks blocks are all unused;
     block 0 is given out first."""
@@ -178,15 +202,7 @@ def extend(context_lens, new_lens, block_table, free_blocks, free_state, T, bloc
     if given, else a new one).  ``block_table`` and ``free_state`` are updated in
     place; a request whose total_lens is not context_lens + new_lens was refused."""
     torch = _torch()
-    i32 = torch.int32
-    dev, index = _gpu(block_table, "block_table")
-    B = context_lens.numel()
-    _want(context_lens, "context_lens", i32, (B,), dev, index)
-    _want(new_lens, "new_lens", i32, (B,), dev, index)
-    stride = _table(block_table, B, dev, index)
-    nb = free_blocks.numel()
-    _want(free_blocks, "free_blocks", i32, (nb,), dev, index)
-    _want(free_state, "free_state", i32, (2,), dev, index)
+    dev, index, B, stride, nb = _blocks(context_lens, new_lens, "new_lens", block_table, free_blocks, free_state)
     if plan is None:
         if T < 0:
             raise ValueError(f"T = {T} is negative")
@@ -196,6 +212,7 @@ def extend(context_lens, new_lens, block_table, free_blocks, free_state, T, bloc
             with torch.cuda.stream(stream):
                 plan = empty_plan(B, T, dev)
     else:
+        i32 = torch.int32
         _want(plan.token_offsets, "token_offsets", i32, (B + 1,), dev, index)
         _want(plan.total_lens, "total_lens", i32, (B,), dev, index)
         _want(plan.slot_mapping, "slot_mapping", torch.int64, (T,), dev, index)
@@ -211,15 +228,7 @@ def release(context_lens, keep_lens, block_table, free_blocks, free_state, block
     """apex_steps_release over torch tensors: the blocks that keep_lens[b] of a
     request's context_lens[b] tokens do not need go back to ``free_blocks``.
     ``block_table``, ``free_blocks`` and ``free_state`` are updated in place."""
-    i32 = _torch().int32
-    dev, index = _gpu(block_table, "block_table")
-    B = context_lens.numel()
-    _want(context_lens, "context_lens", i32, (B,), dev, index)
-    _want(keep_lens, "keep_lens", i32, (B,), dev, index)
-    stride = _table(block_table, B, dev, index)
-    nb = free_blocks.numel()
-    _want(free_blocks, "free_blocks", i32, (nb,), dev, index)
-    _want(free_state, "free_state", i32, (2,), dev, index)
+    _, index, B, stride, nb = _blocks(context_lens, keep_lens, "keep_lens", block_table, free_blocks, free_state)
     _call("apex_steps_release", index, context_lens.data_ptr(), keep_lens.data_ptr(), block_table.data_ptr(), stride,
           free_blocks.data_ptr(), free_state.data_ptr(), B, block_size, nb, _raw_stream(stream, index))
 
@@ -327,5 +336,6 @@ def tree_attention(q, k_new, v_new, token_offsets, tree_mask, k_cache, v_cache, 
     out, lse = _outputs(q, T, Hq, index, out, lse_out, stream)
     _call("apex_steps_tree_attention", index, q.data_ptr(), qs, k_new.data_ptr(), v_new.data_ptr(), ks,
           token_offsets.data_ptr(), tree_mask.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(),
-          stride, context_lens.data_ptr(), out.data_ptr(), lse, B, T, max_nodes, Hq, Hkv, HEAD_DIM, BLOCK_SIZE, shape[0], scale, ws, ws_bytes, _raw_stream(stream, index))
+          stride, context_lens.data_ptr(), out.data_ptr(), lse, B, T, max_nodes, Hq, Hkv, HEAD_DIM, BLOCK_SIZE, shape[0],
+          scale, ws, ws_bytes, _raw_stream(stream, index))
     return out

@@ -59,7 +59,8 @@ def check(results, got, lse, scale):
             empty = np.isneginf(ref)
             assert np.all(np.isneginf(lse[at, h][empty]))
             lt = err + 2.0 ** -22 * (1 + np.abs(ref)) + total
-            off = np.abs(lse[at, h].astype(np.float64) - ref)
+            with np.errstate(invalid="ignore"):
+                off = np.abs(lse[at, h].astype(np.float64) - ref)
             assert np.all(off[~empty] <= lt[~empty]), (at, h, n, off[~empty].max())
     return rows
 
@@ -222,6 +223,67 @@ def test_prompt_long_against_fp32(torch, steps):
         for h in range(Hq):
             one = O.attend(q[r:r + 1, h], k[:r + 1, h // G], v[:r + 1, h // G], SCALE, np.ones((1, r + 1), bool))
             check([(slice(0, 1), 0, r + 1, one)], got[r:r + 1, h:h + 1], lse[r:r + 1, h:h + 1], SCALE)
+
+
+def plain64(torch, q, k, v, offsets, scale):
+    """out, lse and the sums of weight x |V| of packed prompts, in 64 bits on the GPU."""
+    G = q.shape[1] // k.shape[1]
+    out, lse, mag, most = [], [], [], []
+    for lo, hi in zip(offsets[:-1], offsets[1:]):
+        a, b, c = (x[lo:hi].double().transpose(0, 1) for x in (q, k, v))
+        b, c = b.repeat_interleave(G, 0), c.repeat_interleave(G, 0)
+        bt = b.transpose(1, 2).contiguous()
+        s = (a @ bt * scale).masked_fill(torch.ones(hi - lo, hi - lo, dtype=torch.bool, device="cuda").triu(1), -np.inf)
+        w = torch.softmax(s, -1)
+        out.append((w @ c).transpose(0, 1))
+        mag.append((w @ c.abs()).transpose(0, 1))
+        lse.append(torch.logsumexp(s, -1).transpose(0, 1))
+        most.append((a.abs() @ bt.abs()).tril().amax(-1).transpose(0, 1))
+    return [torch.cat(x).cpu().numpy() for x in (out, lse, mag, most)]
+
+
+@pytest.mark.parametrize("B,n,Hq,Hkv", [(64, 200, 32, 32), (40, 300, 16, 16), (20, 300, 32, 8), (7, 500, 64, 32), (150, 70, 12, 12),
+                                        (1, 3000, 64, 8)])
+def test_prompts_of_many_tiles(torch, steps, B, n, Hq, Hkv):
+    """Several tiles a work group: 1 to 14 to a compute unit."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(n // 2, n + 1, B).tolist()
+    lens[-1] = n
+    q, k, v, offsets = prompts(lens, Hq, Hkv, B)
+    got, lse = run_prompts(torch, steps, q, k, v, offsets)
+    out, ref, mag, most = plain64(torch, *dev(torch, q, k, v), offsets.tolist(), SCALE)
+    for h in range(Hq):
+        check([(slice(0, sum(lens)), h, n, (out[:, h], ref[:, h], mag[:, h], most[:, h]))], got, lse, SCALE)
+
+
+def test_attention_refuses_what_it_cannot_read(torch, steps):
+    c = trees([20, 5], [3, 4], 4, 2, 40)
+    a = device(torch, c)
+    q, k, v, o = a[:4]
+    for bad in ((q.float(), k, v, o), (q, k.bfloat16(), v, o), (q[:5], k, v, o), (q, k[:, :1], v, o), (q[..., :64], k, v, o),
+                (q, k, v, o.long()), (q, k, v, o.cpu()), (q.cpu(), k, v, o), (q, k.cpu(), v, o), (q, k, v[:6], o),
+                (q.transpose(1, 2).contiguous().transpose(1, 2), k, v, o), (q, k, torch.cat([v, v], 1)[:, :2], o)):
+        with pytest.raises((ValueError, TypeError)):
+            steps.prompt_attention(*bad, SCALE)
+        with pytest.raises((ValueError, TypeError)):
+            steps.tree_attention(*bad, *a[4:], SCALE)
+    for i, bad in ((4, a[4].int()), (4, a[4][:3]), (5, a[5].float()), (5, a[5][:, :1]), (6, a[6][1:]), (7, a[7].long()),
+                   (7, a[7][:1]), (8, a[8][:1]), (8, a[8].cpu())):
+        with pytest.raises((ValueError, TypeError)):
+            steps.tree_attention(*a[:i], bad, *a[i + 1:], SCALE)
+    for kw in (dict(out=torch.empty_like(q)[:2]), dict(out=q.float()), dict(lse_out=torch.empty(7, 3, device="cuda"))):
+        with pytest.raises((ValueError, TypeError)):
+            steps.prompt_attention(q, k, v, o, SCALE, **kw)
+    import paper_2506_03296_amd as A
+    small = torch.empty(256, dtype=torch.uint8, device="cuda")
+    for kw in (dict(workspace=small),):
+        with pytest.raises(A.ApexError):
+            steps.tree_attention(*a, SCALE, **kw)
+    with pytest.raises(A.ApexError):
+        steps.prompt_attention(q, k, v, o, SCALE, out=q)
+    with pytest.raises(A.ApexError, match="capture"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            steps.tree_attention(*a, SCALE)
 
 
 def test_prompt_captured_and_replayed(torch, steps):

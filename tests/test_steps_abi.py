@@ -99,7 +99,8 @@ BAD, UNSUP = A.APEX_ERR_INVALID_ARG, A.APEX_ERR_UNSUPPORTED
     (tree, dict(lens=None), BAD), (tree, dict(out=None), BAD), (tree, dict(mask=at(6) + 4), BAD),
     (tree, dict(kc=at(7) + 2), BAD), (tree, dict(ws=at(11) + 16, ws_bytes=1 << 40), BAD), (tree, dict(out=at(7) + 4096), BAD),
     (tree, dict(out=at(9)), BAD), (tree, dict(lse=at(10)), BAD), (tree, dict(out=at(6)), BAD),
-    (tree, dict(ks=1000), BAD), (tree, dict(Hq=1 << 22, Hkv=1), UNSUP),
+    (tree, dict(ks=1000), BAD), (tree, dict(Hq=1 << 22, Hkv=1), UNSUP), (tree, dict(Hq=(1 << 16) + 1, Hkv=1), UNSUP),
+    (prompt, dict(Hq=1 << 17, T=100), UNSUP), (prompt, dict(B=1 << 22, Hq=1 << 10, Hkv=1 << 10), UNSUP),
 ])
 def test_refusals(lib, call, kw, rc):
     assert call(lib, **kw) == rc
