@@ -97,7 +97,14 @@ __device__ inline void load_to_lds(const char* from, unsigned to)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane((int)to)), "v"(from) : "memory");
 }
 
-// The same from one address in all lanes and an offset of each, past the caches:
+// The same from one address in all lanes and an offset of each.
+__device__ inline void load_to_lds(const char* from, unsigned offset, unsigned to)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane((int)to)),
+                 "v"(offset), "s"(from) : "memory");
+}
+
+// The same, past the caches:
 // what is read once (a batch of 32 long contexts: 282 us, 315 by way of them).
 __device__ inline void stream_to_lds(const char* from, unsigned offset, unsigned to)
 {

@@ -127,13 +127,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
     // and lane i the piece that belongs at i % 16 of key i / 16.  There are two
     // buffers: a tile is on its way while the one before it is worked on.
     lds_char* const shared = (lds_char*)lds;
+    // Where a tile lies whole inside its request, a lane's offsets from its first row
+    // are the same for all tiles (if a tile's rows span less than 2^31 bytes).
+    const bool near = a.kv_stride < (int64_t)1 << 24;
+    unsigned k_offset[kLoads], v_offset[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+        const unsigned key = wave * 4 + (lane >> 4) + j * 4 * kWaves, row = key * (unsigned)a.kv_stride;
+        k_offset[j] = row + k_piece(key, lane & 15) * 16;
+        v_offset[j] = row + v_piece(key, lane & 15) * 16;
+    }
     const auto load = [&](const Work& w, int t, unsigned buffer) {
         const unsigned to = lds_address(shared) + buffer * 2 * kTileBytes + wave * 1024;
-        const int64_t request0 = (int64_t)w.first * a.kv_stride + w.head * kRowBytes;
+        const int64_t tile0 = (int64_t)(w.first + t * kKeys) * a.kv_stride + w.head * kRowBytes;
+        if (near && (t + 1) * kKeys <= w.n) {
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                load_to_lds(a.k + tile0, k_offset[j], to + j * 4 * kWaves * kRowBytes);
+                load_to_lds(a.v + tile0, v_offset[j], to + kTileBytes + j * 4 * kWaves * kRowBytes);
+            }
+            return;
+        }
+        const unsigned lane = lane_again();
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
             const unsigned key = wave * 4 + (lane >> 4) + j * 4 * kWaves;
-            const int64_t at = request0 + (int64_t)(t * kKeys + (int)key) * a.kv_stride;
+            const int64_t at = tile0 + (int64_t)key * a.kv_stride;
             const char* k = a.k + at + k_piece(key, lane & 15) * 16;
             const char* v = a.v + at + v_piece(key, lane & 15) * 16;
             if (t * kKeys + (int)key >= w.n) k = v = (const char*)kZeros;     // behind the request
