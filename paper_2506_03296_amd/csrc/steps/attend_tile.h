@@ -131,58 +131,53 @@ __device__ inline void barrier()
 
 __device__ inline unsigned lds_address(const lds_char* p) { return (unsigned)(uintptr_t)p; }
 
-// One wave's rows, kTiles tiles of 32; kSub tiles of 32 keys are taken at a time.
-template <int kSub, int kTiles = 1>
+// One wave's 32 rows; kSub tiles of 32 keys are taken at a time.
+template <int kSub>
 struct Rows {
-    f16x8 q[kTiles][8];      // lane n and n + 32: row n, dims 16 j + 8 (lane / 32) + 0..7 in q[][j]
-    f32x16 o[kTiles][4];     // O^T, dims 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4 in o[][t][i], times 2^kBias
-    float top[kTiles];       // M
-    float sum[kTiles];       // of this lane's half of the keys
+    f16x8 q[8];          // lane n and n + 32: row n, dims 16 j + 8 (lane / 32) + 0..7 in q[j]
+    f32x16 o[4];         // O^T, dims 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4 in o[t][i], times 2^kBias
+    float top;           // M
+    float sum;           // of this lane's half of the keys
 
-    // Row pointer of the lane's query of tile r, or NULL: a row of zeros.
-    __device__ void start(int r, const char* row)
+    // Row pointer of the lane's query, or NULL: a row of zeros.
+    __device__ void start(const char* row)
     {
         const unsigned half = (threadIdx.x & 63) >> 5;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             u32x4 x = {0u, 0u, 0u, 0u};
             if (row) x = *(const u32x4*)(row + j * 32 + half * 16);
-            q[r][j] = __builtin_bit_cast(f16x8, x);
+            q[j] = __builtin_bit_cast(f16x8, x);
         }
     }
 
-    // The lane's query of tile r out of rows in LDS that lie as K's.
-    __device__ void read_q(int r, const lds_char* rows)
+    // The lane's query out of rows in LDS that lie as K's.
+    __device__ void read_q(const lds_char* rows)
     {
         const unsigned lane = lane_again(), row = lane & 31, half = lane >> 5;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[r][j] = *(const lds_f16x8*)(rows + row * kRowBytes + k_piece(row, 2 * j + half) * 16);
+        for (int j = 0; j < 8; ++j) q[j] = *(const lds_f16x8*)(rows + row * kRowBytes + k_piece(row, 2 * j + half) * 16);
     }
 
     // A negative scale is taken as its magnitude, with q's sign turned.
     __device__ void negate()
     {
 #pragma unroll
-        for (int r = 0; r < kTiles; ++r)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q[r][j] = __builtin_bit_cast(f16x8, __builtin_bit_cast(u32x4, q[r][j]) ^ 0x80008000u);
+            for (int j = 0; j < 8; ++j) q[j] = __builtin_bit_cast(f16x8, __builtin_bit_cast(u32x4, q[j]) ^ 0x80008000u);
     }
 
     __device__ void clear()
     {
 #pragma unroll
-        for (int r = 0; r < kTiles; ++r) {
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[r][t][i] = 0.0f;
-            top[r] = -INFINITY;
-            sum[r] = 0.0f;
-        }
+            for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
+        top = -INFINITY;
+        sum = 0.0f;
     }
 
-    // Scores of the tiles' keys: key 32 u + 8 (i / 4) + 4 (lane / 32) + i % 4 in s[][u][i].
-    __device__ void scores(const lds_char* k, f32x16 (&s)[kTiles][kSub]) const
+    // Scores of the tiles' keys: key 32 u + 8 (i / 4) + 4 (lane / 32) + i % 4 in s[u][i].
+    __device__ void scores(const lds_char* k, f32x16 (&s)[kSub]) const
     {
         const unsigned lane = threadIdx.x & 63, key = lane & 31, half = lane >> 5;
         f16x8 a[kSub][8];
@@ -193,18 +188,14 @@ struct Rows {
                 a[u][j] = *(const lds_f16x8*)(k + (key + 32 * u) * kRowBytes + k_piece(key, 2 * j + half) * 16);
         __builtin_amdgcn_sched_barrier(0);      // all reads are on their way before the first product waits
 #pragma unroll
-        for (int r = 0; r < kTiles; ++r)
-#pragma unroll
             for (int u = 0; u < kSub; ++u)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[r][u][i] = 0.0f;
+                for (int i = 0; i < 16; ++i) s[u][i] = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int u = 0; u < kSub; ++u)
-#pragma unroll
-                for (int r = 0; r < kTiles; ++r)
-                    s[r][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][j], q[r][j], s[r][u], 0, 0, 0);
+                    s[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[u][j], q[j], s[u], 0, 0, 0);
     }
 
     // Takes out the scores of keys that the lane's query does not see: bit j of
@@ -221,8 +212,8 @@ struct Rows {
         }
     }
 
-    // The running maximum of tile r after these scores.
-    __device__ void raise(int r, const f32x16 (&s)[kSub], float c)
+    // The running maximum after these scores.
+    __device__ void raise(const f32x16 (&s)[kSub], float c)
     {
         float m[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};      // four chains
 #pragma unroll
@@ -230,14 +221,14 @@ struct Rows {
 #pragma unroll
             for (int i = u ? 0 : 4; i < 16; ++i) m[i & 3] = fmaxf(m[i & 3], s[u][i]);
         const float most = max_of_halves(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]))) * c;
-        if (__builtin_expect(__any(most > top[r] + kSlack), 0)) rescale(r, fmaxf(most, top[r]));
+        if (__builtin_expect(__any(most > top + kSlack), 0)) rescale(fmaxf(most, top));
     }
 
-    // Weights of 32 keys' scores of tile r, as P^T's operands: keys 16 w + 4 half + 0..3 and + 8 in p[w].
-    __device__ void weights(int r, const f32x16& s, float c, f16x8* p)
+    // Weights of 32 keys' scores, as P^T's operands: keys 16 w + 4 half + 0..3 and + 8 in p[w].
+    __device__ void weights(const f32x16& s, float c, f16x8* p)
     {
         // a row that has seen no score yet keeps M = -inf: 2^(-inf - 0) = 0
-        const float base = (top[r] == -INFINITY ? 0.0f : top[r]) - kBias;
+        const float base = (top == -INFINITY ? 0.0f : top) - kBias;
         float part[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < 2; ++w)
@@ -252,18 +243,18 @@ struct Rows {
                 p[w][j] = h[0];
                 p[w][j + 1] = h[1];
             }
-        sum[r] += part[0] + part[1];
+        sum += part[0] + part[1];
     }
 
-    __device__ void rescale(int r, float to)
+    __device__ void rescale(float to)
     {
-        const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top[r] - to);
-        sum[r] *= f;
+        const float f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(top - to);
+        sum *= f;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[r][t][i] *= f;
-        top[r] = to;
+            for (int i = 0; i < 16; ++i) o[t][i] *= f;
+        top = to;
     }
 
     // V^T's operand: dims 32 t + lane % 32, the 16 keys of step w in P^T's order.
@@ -287,33 +278,27 @@ struct Rows {
         __builtin_amdgcn_sched_barrier(0);
     }
 
-    __device__ void add(int r, const f16x8 (&a)[2][4], const f16x8* p)
+    __device__ void add(const f16x8 (&a)[2][4], const f16x8* p)
     {
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) o[r][t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[w][t], p[w], o[r][t], 0, 0, 0);
+            for (int t = 0; t < 4; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[w][t], p[w], o[t], 0, 0, 0);
     }
 
     // The weights of a unit's scores and their products with V: V's operands come
     // while weights are made, and the weights of 32 keys are made while the matrix
     // cores work on the 32 before them.
-    __device__ void take(const f32x16 (&s)[kTiles][kSub], float c, const lds_char* v)
+    __device__ void take(const f32x16 (&s)[kSub], float c, const lds_char* v)
     {
 #pragma unroll
         for (int u = 0; u < kSub; ++u) {
             f16x8 a[2][4];
             read_v(v, u, a);
-            if (u == 0) {
-#pragma unroll
-                for (int r = 0; r < kTiles; ++r) raise(r, s[r], c);
-            }
-#pragma unroll
-            for (int r = 0; r < kTiles; ++r) {
-                f16x8 p[2];
-                weights(r, s[r][u], c, p);
-                add(r, a, p);
-            }
+            if (u == 0) raise(s, c);
+            f16x8 p[2];
+            weights(s[u], c, p);
+            add(a, p);
         }
     }
 
@@ -324,16 +309,14 @@ struct Rows {
     {
         float x = 0.0f;
 #pragma unroll
-        for (int r = 0; r < kTiles; ++r)
-#pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x += o[r][t][i];
+                for (int i = 0; i < 16; ++i) x += o[t][i];
         return __any(!(fabsf(x) < INFINITY));
     }
 
-    // One key, by its rows in global memory (this kv-head's), for the queries of tile r that see it.
-    __device__ void take_key(int r, const char* k, const char* v, float c, bool sees)
+    // One key, by its rows in global memory (this kv-head's), for the queries that see it.
+    __device__ void take_key(const char* k, const char* v, float c, bool sees)
     {
         const unsigned half = (threadIdx.x & 63) >> 5;
         float dot = 0.0f;
@@ -342,23 +325,23 @@ struct Rows {
             const f16x8 x = *(const f16x8*)(k + j * 32 + half * 16);
 #pragma unroll
             for (int i = 0; i < 8; i += 2)
-                dot = __builtin_amdgcn_fdot2(f16x2{x[i], x[i + 1]}, f16x2{q[r][j][i], q[r][j][i + 1]}, dot, false);
+                dot = __builtin_amdgcn_fdot2(f16x2{x[i], x[i + 1]}, f16x2{q[j][i], q[j][i + 1]}, dot, false);
             asm volatile("" ::: "memory");      // one load at a time: this path may not cost the other registers
         }
         dot = sum_of_halves(dot);
         const float m = sees ? dot * c : -INFINITY;
-        if (__any(m > top[r] + kSlack)) rescale(r, fmaxf(m, top[r]));
-        const float base = (top[r] == -INFINITY ? 0.0f : top[r]) - kBias;
+        if (__any(m > top + kSlack)) rescale(fmaxf(m, top));
+        const float base = (top == -INFINITY ? 0.0f : top) - kBias;
         const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, c, -base));
         if (!sees) return;
-        if (half == 0) sum[r] += e;
+        if (half == 0) sum += e;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const f16x4 x = *(const f16x4*)(v + t * 64 + i * 16 + half * 8);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o[r][t][4 * i + j] = __builtin_fmaf(e, (float)x[j], o[r][t][4 * i + j]);
+                for (int j = 0; j < 4; ++j) o[t][4 * i + j] = __builtin_fmaf(e, (float)x[j], o[t][4 * i + j]);
                 asm volatile("" ::: "memory");
             }
     }

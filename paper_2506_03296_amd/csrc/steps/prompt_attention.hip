@@ -200,7 +200,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
     load_q(w);
     load(w, 0, 0);
     arrived<0>();
-    r.read_q(0, own);
+    r.read_q(own);
     for (unsigned buffer = 0;;) {
         // the item's first tile and q have arrived; the results of the one before lie in `own`
         barrier();
@@ -228,11 +228,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
         for (; t < own_tiles; ++t) {
             bring(t);
             const lds_char* kt = shared + buffer * 2 * kTileBytes;
-            f32x16 s[1][2];
+            f32x16 s[2];
             r.scores(kt, s);
             if ((t + 1) * kKeys > wave_lo + 1) {
                 const int seen = pos - t * kKeys + 1;       // keys of the tile up to the row's own
-                r.mask(s[0], seen >= 64 ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
+                r.mask(s, seen >= 64 ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
             }
             r.take(s, a.c, kt + kTileBytes);
             buffer ^= 1;
@@ -254,21 +254,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
 #pragma nounroll
             for (int key = 0; key <= wave_hi; ++key) {
                 const int64_t at = (int64_t)(w.first + key) * a.kv_stride + w.head * kRowBytes;
-                r.take_key(0, a.k + at, a.v + at, a.c, key <= pos);
+                r.take_key(a.k + at, a.v + at, a.c, key <= pos);
             }
         }
         if (more) {
             arrived<0>();
-            r.read_q(0, own);
+            r.read_q(own);
         }
-        const float sum = sum_of_halves(r.sum[0]), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        lse = (r.top[0] - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
+        const float sum = sum_of_halves(r.sum), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        lse = (r.top - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
         const unsigned in = lane_again() & 31, upper = lane_again() >> 5;
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const f32x4 x = {r.o[0][d][4 * i] * inv, r.o[0][d][4 * i + 1] * inv, r.o[0][d][4 * i + 2] * inv, r.o[0][d][4 * i + 3] * inv};
+                const f32x4 x = {r.o[d][4 * i] * inv, r.o[d][4 * i + 1] * inv, r.o[d][4 * i + 2] * inv, r.o[d][4 * i + 3] * inv};
                 *(lds_f16x4*)(own + in * kRowBytes + k_piece(in, 4 * d + i) * 16 + upper * 8) =
                     __builtin_convertvector(x, f16x4);
             }

@@ -68,14 +68,15 @@ __device__ inline int request_cost(const Args& a, const Request& r)
     return r.nodes ? a.Hkv * r.tiles * (r.units + kPairCost) : 0;
 }
 
-// kRowWaves waves hold kTiles tiles of 32 rows each, kWaves / kRowWaves waves share
-// their keys, 32 kSub each of a unit.
-template <int kTiles_, int kRowWaves_, int kSub_, int kWaves_>
+// Eight waves: kRowWaves of them hold 32 rows each, kParts of them share a row tile's
+// keys, 32 kSub each of a unit.
+constexpr int kWaves = 8;
+template <int kRowWaves_, int kSub_>
 struct Shape {
-    static constexpr int kTiles = kTiles_, kRowWaves = kRowWaves_, kSub = kSub_, kWaves = kWaves_;
+    static constexpr int kRowWaves = kRowWaves_, kSub = kSub_;
     static constexpr int kParts = kWaves / kRowWaves;
     static constexpr int kWaveKeys = 32 * kSub, kKeys = kParts * kWaveKeys;
-    static constexpr int kWaveTile = kTiles * kWaveRows, kTileRows = kRowWaves * kWaveTile;
+    static constexpr int kTileRows = kRowWaves * kWaveRows;
     static constexpr int kBytes = kKeys * kRowBytes;             // of a unit's K or V
     // A wave brings the keys that it takes and no others, into one buffer, each half
     // of which it fills again as soon as it has read it (kOwn), or the work group's
@@ -86,7 +87,7 @@ struct Shape {
     static constexpr int kPartBlocks = kWaveKeys / kBlockSize;   // blocks of a wave's keys
     // Parts' sums are joined by way of the buffer that the last unit has left (of
     // kOwn its half for V), in rounds.
-    static constexpr int kRounds = kParts == 1 ? 1 : kWaves * kWaveTile * kHeadDim * 4 / ((kOwn ? 1 : 2) * kBytes);
+    static constexpr int kRounds = kParts == 1 ? 1 : kWaves * kWaveRows * kHeadDim * 4 / ((kOwn ? 1 : 2) * kBytes);
     static_assert(kParts == 1 || kRounds == 1 || kRounds == 2 || kRounds == 4, "a round takes 128 / kRounds dims");
 };
 
@@ -97,13 +98,13 @@ struct Segment {
 };
 
 template <class S>
-__global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
+__global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
 {
-    constexpr int kTiles = S::kTiles, kParts = S::kParts, kWaveKeys = S::kWaveKeys, kKeys = S::kKeys, kLoads = S::kLoads;
+    constexpr int kParts = S::kParts, kWaveKeys = S::kWaveKeys, kKeys = S::kKeys, kLoads = S::kLoads;
     constexpr int kTileRows = S::kTileRows, kBytes = S::kBytes, kSub = S::kSub;
     constexpr bool kOwn = S::kOwn;
     __shared__ __attribute__((aligned(16))) char lds[S::kLds];
-    __shared__ float merge_top[S::kWaves][S::kWaveTile], merge_sum[S::kWaves][S::kWaveTile];
+    __shared__ float merge_top[kWaves][kWaveRows], merge_sum[kWaves][kWaveRows];
 
     const unsigned lane = threadIdx.x & 63, wave = (unsigned)uniform((int)(threadIdx.x >> 6));
     const unsigned half = lane >> 5;
@@ -183,7 +184,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
     constexpr int kIds = kOwn ? kLoads / 4 : kLoads;
     int ids[kIds], part_ids[S::kPartBlocks];             // of the blocks of the unit that is asked for next
     const unsigned block_bytes = (unsigned)a.Hkv * kSlabBytes, num_blocks = (unsigned)a.num_blocks;
-    const auto first_key = [&](int j) { return kOwn ? (int)wave * kWaveKeys + j * 4 : (j * S::kWaves + (int)wave) * 4; };
+    const auto first_key = [&](int j) { return kOwn ? (int)wave * kWaveKeys + j * 4 : (j * kWaves + (int)wave) * 4; };
     const auto id_of = [&](const Segment& g, const int32_t* row, int u, int key) {
         const int e = u * (kKeys / kBlockSize) + key / kBlockSize;
         return u < g.cached && e * kBlockSize < g.q.len ? row[e] : -1;
@@ -245,27 +246,24 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
             if ((unsigned)part_ids[j] < num_blocks) bits |= 1u << j;
         return bits;
     };
-    Rows<kSub, kTiles> r;
-    uint64_t tree[kTiles];                               // the drafted tokens that the lane's rows see
-    const auto row_of = [&](const Segment& g, int i) {
-        return (unsigned)(g.tile * kTileRows + row_wave * S::kWaveTile + i * kWaveRows) + (lane_again() & 31);
+    Rows<kSub> r;
+    uint64_t tree;                                       // the drafted tokens that the lane's rows see
+    const auto row_of = [&](const Segment& g) {
+        return (unsigned)(g.tile * kTileRows + row_wave * kWaveRows) + (lane_again() & 31);
     };
-    const auto rows = [&](const Segment& g, uint64_t (&words)[kTiles]) {
+    const auto rows = [&](const Segment& g) {
         const Arguments f = arguments();
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) {
-            const unsigned row = row_of(g, i), G = f->G.d, node = divide(row, f->G);
-            const bool live = (int)node < g.q.nodes;
-            r.start(i, live ? f->q + (int64_t)(g.q.first + (int)node) * f->q_stride + (g.kv_head * G + row - node * G) * kRowBytes
-                            : nullptr);
-            words[i] = live ? f->mask[g.q.first + (int)node] : 0;
-        }
+        const unsigned row = row_of(g), G = f->G.d, node = divide(row, f->G);
+        const bool live = (int)node < g.q.nodes;
+        r.start(live ? f->q + (int64_t)(g.q.first + (int)node) * f->q_stride + (g.kv_head * G + row - node * G) * kRowBytes
+                     : nullptr);
+        tree = live ? f->mask[g.q.first + (int)node] : 0;
     };
 
     Segment g, ahead;
     if (!next(g)) return;
     ask(g, g.lo);
-    rows(g, tree);
+    rows(g);
     r.clear();
     unsigned there = present(), buffer = 0;
     load(g, g.lo, 0, false);
@@ -292,7 +290,7 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
             }
         }
         lds_char* const kt = shared + (kOwn ? 0 : buffer * 2 * kBytes) + from * kRowBytes;
-        f32x16 s[kTiles][kSub];
+        f32x16 s[kSub];
         r.scores(kt, s);
         if (kOwn && more) {
             was_read();
@@ -305,14 +303,10 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
                 if (there >> j & 1) allow |= 0xffffull << (16 * j);
             const int n = g.q.len - u * kKeys - from;
             allow &= n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
-            if (allow != (kSub == 2 ? ~0ull : 0xffffffffull)) {
-#pragma unroll
-                for (int i = 0; i < kTiles; ++i) r.mask(s[i], allow);
-            }
+            if (allow != (kSub == 2 ? ~0ull : 0xffffffffull)) r.mask(s, allow);
         } else {
             const uint64_t nodes = from >= 64 ? 0 : (g.q.nodes >= 64 ? ~0ull : (1ull << g.q.nodes) - 1) >> from;
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i) r.mask(s[i], tree[i] >> (from & 63) & nodes);
+            r.mask(s, tree >> (from & 63) & nodes);
         }
         if (kOwn) {
             if (more) arrived<kLoads>();                 // V; the next K is on its way
@@ -354,99 +348,79 @@ __global__ __launch_bounds__(64 * S::kWaves, 2) void tree_kernel(TreeArgs a)
                     v_row = out->v_new + to;
                     is_there = true;
                 }
-#pragma unroll
-                for (int j = 0; j < kTiles; ++j)
-                    r.take_key(j, k_row, v_row, c, is_there && (v < g.cached || (tree[j] >> (key & 63) & 1)));
+                r.take_key(k_row, v_row, c, is_there && (v < g.cached || (tree >> (key & 63) & 1)));
             }
         }
-        if (more) rows(ahead, tree);                     // on their way while the parts meet
+        if (more) rows(ahead);                           // on their way while the parts meet
 
         // the parts' sums together, each wave of a tile some of the dims
         lds_char* const meet = shared + (kOwn ? kBytes : buffer * 2 * kBytes);
         const bool whole = g.lo == 0 && g.hi == g.q.units;
         const int64_t slot = 2 * (int64_t)blockIdx.x + (g.lo == 0 ? 1 : 0);
-        float top[kTiles], sum[kTiles], f[kTiles][kParts];
-#pragma unroll
-        for (int n = 0; n < kTiles; ++n) {
-            top[n] = r.top[n];
-            sum[n] = sum_of_halves(r.sum[n]);
-        }
+        float top = r.top, sum = sum_of_halves(r.sum), f[kParts];
         if (kParts > 1) {
             if (half == 0) {
-#pragma unroll
-                for (int n = 0; n < kTiles; ++n) {
-                    merge_top[wave][n * kWaveRows + lane] = top[n];
-                    merge_sum[wave][n * kWaveRows + lane] = sum[n];
-                }
+                merge_top[wave][lane] = top;
+                merge_sum[wave][lane] = sum;
             }
             barrier();
+            top = -INFINITY;
+            sum = 0.0f;
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) {
-                const int i = n * kWaveRows + (lane & 31);
-                top[n] = -INFINITY;
-                sum[n] = 0.0f;
+            for (int w = 0; w < kParts; ++w) {
+                f[w] = merge_top[w * S::kRowWaves + row_wave][lane & 31];
+                top = fmaxf(top, f[w]);
+            }
 #pragma unroll
-                for (int w = 0; w < kParts; ++w) {
-                    f[n][w] = merge_top[w * S::kRowWaves + row_wave][i];
-                    top[n] = fmaxf(top[n], f[n][w]);
-                }
-#pragma unroll
-                for (int w = 0; w < kParts; ++w) {
-                    f[n][w] = f[n][w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(f[n][w] - top[n]);
-                    sum[n] = __builtin_fmaf(f[n][w], merge_sum[w * S::kRowWaves + row_wave][i], sum[n]);
-                }
+            for (int w = 0; w < kParts; ++w) {
+                f[w] = f[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(f[w] - top);
+                sum = __builtin_fmaf(f[w], merge_sum[w * S::kRowWaves + row_wave][lane & 31], sum);
             }
         }
+        const unsigned row = row_of(g), G = out->G.d, node = divide(row, out->G);
+        const bool live = (int)node < g.q.nodes;
+        const int64_t to = (int64_t)(g.q.first + (int)node) * out->Hq + g.kv_head * G + row - node * G;
+        const int64_t in_slot = slot * kTileRows + row_wave * kWaveRows + (lane & 31);
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
         for (int round = 0; round < S::kRounds; ++round) {
             constexpr int kQuads = 16 / S::kRounds;      // of 4 dims a lane, of a round
             if (kParts > 1) {
                 if (round) barrier();
 #pragma unroll
-                for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-                    for (int i = 0; i < kQuads; ++i) {
-                        const int t = (round * kQuads + i) / 4, e = (round * kQuads + i) % 4 * 4;
-                        *(lds_f32x4*)(meet + (((wave * kTiles + n) * kQuads + i) * 64 + lane) * 16) =
-                            f32x4{r.o[n][t][e], r.o[n][t][e + 1], r.o[n][t][e + 2], r.o[n][t][e + 3]};
-                    }
+                for (int i = 0; i < kQuads; ++i) {
+                    const int t = (round * kQuads + i) / 4, e = (round * kQuads + i) % 4 * 4;
+                    *(lds_f32x4*)(meet + ((wave * kQuads + i) * 64 + lane) * 16) =
+                        f32x4{r.o[t][e], r.o[t][e + 1], r.o[t][e + 2], r.o[t][e + 3]};
+                }
                 barrier();
             }
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) {
-                const unsigned row = row_of(g, n), G = out->G.d, node = divide(row, out->G);
-                const bool live = (int)node < g.q.nodes;
-                const int64_t to = (int64_t)(g.q.first + (int)node) * out->Hq + g.kv_head * G + row - node * G;
-                const int64_t in_slot = slot * kTileRows + row_wave * S::kWaveTile + n * kWaveRows + (lane & 31);
-                const float inv = sum[n] == 0.0f ? 0.0f : 1.0f / sum[n];
+            for (int i = 0; i < kQuads; ++i) {
+                if (kParts > 1 && i / (kQuads / kParts) != part) continue;
+                const int t = (round * kQuads + i) / 4, e = (round * kQuads + i) % 4;
+                f32x4 y = {r.o[t][4 * e], r.o[t][4 * e + 1], r.o[t][4 * e + 2], r.o[t][4 * e + 3]};
+                if (kParts > 1) {
+                    y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int i = 0; i < kQuads; ++i) {
-                    if (kParts > 1 && i / (kQuads / kParts) != part) continue;
-                    const int t = (round * kQuads + i) / 4, e = (round * kQuads + i) % 4;
-                    f32x4 y = {r.o[n][t][4 * e], r.o[n][t][4 * e + 1], r.o[n][t][4 * e + 2], r.o[n][t][4 * e + 3]};
-                    if (kParts > 1) {
-                        y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                    for (int w = 0; w < kParts; ++w) {
+                        const f32x4 z = *(const lds_f32x4*)(meet + (((w * S::kRowWaves + row_wave) * kQuads + i) * 64 + lane) * 16);
 #pragma unroll
-                        for (int w = 0; w < kParts; ++w) {
-                            const f32x4 z = *(const lds_f32x4*)(
-                                meet + ((((w * S::kRowWaves + row_wave) * kTiles + n) * kQuads + i) * 64 + lane) * 16);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) y[j] = __builtin_fmaf(f[n][w], z[j], y[j]);
-                        }
-                    }
-                    if (!live) continue;
-                    if (whole) {
-                        y = f32x4{y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
-                        *(f16x4*)(out->out + to * kRowBytes + t * 64 + e * 16 + half * 8) = __builtin_convertvector(y, f16x4);
-                    } else {
-                        *(f32x4*)(out->sums + in_slot * kHeadDim + t * 32 + e * 8 + half * 4) = y;
+                        for (int j = 0; j < 4; ++j) y[j] = __builtin_fmaf(f[w], z[j], y[j]);
                     }
                 }
-                if (round == 0 && live && part == 0 && half == 0) {
-                    if (!whole) *(f32x2*)(out->tops + in_slot * 2) = f32x2{top[n], sum[n]};
-                    else if (out->lse) out->lse[to] = (top[n] - kBias + __builtin_amdgcn_logf(sum[n])) * kLn2;
+                if (!live) continue;
+                if (whole) {
+                    y = f32x4{y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv};
+                    *(f16x4*)(out->out + to * kRowBytes + t * 64 + e * 16 + half * 8) = __builtin_convertvector(y, f16x4);
+                } else {
+                    *(f32x4*)(out->sums + in_slot * kHeadDim + t * 32 + e * 8 + half * 4) = y;
                 }
             }
+        }
+        if (live && part == 0 && half == 0) {
+            if (!whole) *(f32x2*)(out->tops + in_slot * 2) = f32x2{top, sum};
+            else if (out->lse) out->lse[to] = (top - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
         }
         if (!whole && g.lo == 0 && threadIdx.x == 0) {
             // the parts: this one and those of the next work groups up to the pair's end
@@ -501,10 +475,10 @@ __global__ __launch_bounds__(256) void join_kernel(TreeArgs a, int tile_rows)
 }
 
 // Shapes by the most rows of a pair.
-using Shape32 = Shape<1, 1, 1, 8>;
-using Shape64 = Shape<1, 2, 1, 8>;
-using Shape128 = Shape<1, 4, 2, 8>;
-using Shape256 = Shape<1, 8, 2, 8>;
+using Shape32 = Shape<1, 1>;
+using Shape64 = Shape<2, 1>;
+using Shape128 = Shape<4, 2>;
+using Shape256 = Shape<8, 2>;
 
 int tile_rows(int max_nodes, int G)
 {
@@ -644,10 +618,9 @@ int apex_steps_tree_attention(const void* q, int64_t q_token_stride, const void*
     a.c = (scale < 0 ? -scale : scale) * kLog2e;
     a.negate = scale < 0;
     const hipStream_t on = (hipStream_t)stream;
-    if (rows == 32) tree_kernel<Shape32><<<groups, 64 * Shape32::kWaves, 0, on>>>(a);
-    else if (rows == 64) tree_kernel<Shape64><<<groups, 64 * Shape64::kWaves, 0, on>>>(a);
-    else if (rows == 128) tree_kernel<Shape128><<<groups, 64 * Shape128::kWaves, 0, on>>>(a);
-    else tree_kernel<Shape256><<<groups, 64 * Shape256::kWaves, 0, on>>>(a);
+    const auto kernel = rows == 32 ? tree_kernel<Shape32> : rows == 64 ? tree_kernel<Shape64>
+                        : rows == 128 ? tree_kernel<Shape128> : tree_kernel<Shape256>;
+    kernel<<<groups, 64 * kWaves, 0, on>>>(a);
     rc = launched("tree_attention");
     if (rc != APEX_OK) return rc;
     join_kernel<<<dim3(groups, rows / 8), 256, 0, on>>>(a, rows);
