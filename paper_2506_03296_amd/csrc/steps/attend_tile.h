@@ -50,6 +50,7 @@ typedef __attribute__((address_space(3))) f16x8 lds_f16x8;
 typedef __attribute__((address_space(3))) f16x4 lds_f16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+typedef __attribute__((address_space(3))) f32x2 lds_f32x2;
 
 // Where 16-byte piece c of a key's row lies among the row's 16 pieces.  K is
 // read with 32 neighbouring keys at one piece each: their pieces are spread over

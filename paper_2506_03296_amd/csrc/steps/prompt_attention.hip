@@ -6,8 +6,8 @@ namespace steps {
 
 namespace {
 
-constexpr int kKeys = 64;                        // keys of a tile
-constexpr int kTileBytes = kKeys * kRowBytes;    // of K or of V
+constexpr int kWaves = 8;
+constexpr int kPartKeys = 64;                    // keys of a tile that a wave takes
 constexpr int kSortedRequests = 64;              // requests a wave sorts, one a lane
 
 struct PromptArgs {
@@ -98,14 +98,18 @@ struct Tiles {
 // first tile and rows are asked for before the item before it ends.  The cheapest
 // items that remain have a work group each, which the hardware starts where the
 // others end first.
-template <int kWaves>
+// Eight waves: kRowWaves of them hold 32 rows each, the other half's, if there is
+// one, are the same rows and every second 64 keys.
+template <int kParts>
 __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, unsigned slots, unsigned groups, unsigned rounds)
 {
-    constexpr int kThreads = 64 * kWaves, kRows = kWaveRows * kWaves;
-    constexpr int kLoads = kTileBytes / (kThreads * 16);     // of K, and of V, that bring a tile
+    constexpr int kRowWaves = kWaves / kParts, kRows = kWaveRows * kRowWaves;
+    constexpr int kKeys = kParts * kPartKeys, kTileBytes = kKeys * kRowBytes;     // of a tile; of its K or V
+    constexpr int kLoads = kTileBytes / (64 * kWaves * 16);     // of K, and of V, that bring a tile
     __shared__ __attribute__((aligned(16))) char lds[2 * 2 * kTileBytes + kRows * kRowBytes];
 
     const unsigned lane = threadIdx.x & 63, wave = (unsigned)uniform((int)(threadIdx.x >> 6));
+    const unsigned row_wave = wave % kRowWaves, part = kParts == 1 ? 0 : wave / kRowWaves;
     Tiles<kRows> all;
     all.start(a);
     unsigned round = 0;
@@ -161,9 +165,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
         }
     };
     Rows<2> r;
-    const auto row0 = [&](const Work& w) { return (unsigned)w.tile * kRows + wave * kWaveRows; };      // the wave's first row
+    const auto row0 = [&](const Work& w) { return (unsigned)w.tile * kRows + row_wave * kWaveRows; };      // the wave's first row
     // The wave's rows of q and its results share a piece of LDS: rows of 256 bytes, laid out as K's.
-    lds_char* const own = shared + 4 * kTileBytes + wave * kWaveRows * kRowBytes;
+    lds_char* const own = shared + 4 * kTileBytes + row_wave * kWaveRows * kRowBytes;
     const auto load_q = [&](const Work& w) {
         const unsigned n_rows = (unsigned)w.n * a.G.d, lane = lane_again();
 #pragma unroll
@@ -173,6 +177,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
                             + k_piece(i, lane & 15) * 16;
             load_to_lds(row < n_rows ? q : (const char*)kZeros, lds_address(own) + j * 4 * kRowBytes);
         }
+    };
+
+    // With parts two waves have the same rows, once: straight from global memory.
+    const auto rows = [&](const Work& w) {
+        const unsigned row = row0(w) + (lane_again() & 31), pos = divide(row, a.G);
+        r.start(row < (unsigned)w.n * a.G.d
+                    ? a.q + (int64_t)(w.first + (int)pos) * a.q_stride + (w.head * a.G.d + row - pos * a.G.d) * kRowBytes
+                    : nullptr);
     };
 
     // An item's results wait in LDS until the next one's first tile is worked on:
@@ -197,16 +209,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
     Work w, ahead, before;
     bool have = next(w), stored = true;
     if (!have) return;
-    load_q(w);
+    if (kParts == 1) load_q(w);
+    else rows(w);
     load(w, 0, 0);
     arrived<0>();
-    r.read_q(own);
+    if (kParts == 1) r.read_q(own);
     for (unsigned buffer = 0;;) {
         // the item's first tile and q have arrived; the results of the one before lie in `own`
         barrier();
-        if (!stored) store(before);
+        if (!stored && part == 0) store(before);
         if (!have) return;
-        const bool more = next(ahead);
+        const bool more = kParts == 1 && next(ahead);
         // positions of the wave's and the work group's rows
         const unsigned last_row = (unsigned)w.n * a.G.d - 1;
         const int wave_lo = (int)divide(min(row0(w), last_row), a.G), wave_hi = (int)divide(min(row0(w) + 31, last_row), a.G);
@@ -227,11 +240,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
         int t = 0;
         for (; t < own_tiles; ++t) {
             bring(t);
-            const lds_char* kt = shared + buffer * 2 * kTileBytes;
+            const lds_char* kt = shared + buffer * 2 * kTileBytes + part * kPartKeys * kRowBytes;
+            const int own_t = t * kParts + (int)part;       // the wave's keys, in 64s
             f32x16 s[2];
             r.scores(kt, s);
-            if ((t + 1) * kKeys > wave_lo + 1) {
-                const int seen = pos - t * kKeys + 1;       // keys of the tile up to the row's own
+            if ((own_t + 1) * kPartKeys > wave_lo + 1) {
+                const int seen = pos - own_t * kPartKeys + 1;       // of them, those up to the row's own
                 r.mask(s, seen >= 64 ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
             }
             r.take(s, a.c, kt + kTileBytes);
@@ -253,6 +267,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
             r.clear();
 #pragma nounroll
             for (int key = 0; key <= wave_hi; ++key) {
+                if (kParts == 2 && (unsigned)key / kPartKeys % 2 != part) key += kPartKeys;
+                if (key > wave_hi) break;
                 const int64_t at = (int64_t)(w.first + key) * a.kv_stride + w.head * kRowBytes;
                 r.take_key(a.k + at, a.v + at, a.c, key <= pos);
             }
@@ -261,17 +277,59 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
             arrived<0>();
             r.read_q(own);
         }
-        const float sum = sum_of_halves(r.sum), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        lse = (r.top - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
-        const unsigned in = lane_again() & 31, upper = lane_again() >> 5;
+        float sum = sum_of_halves(r.sum);
+        if (kParts == 2) {
+            // the second part's sums to the first, by way of the buffer that the last
+            // tile has left, in two rounds
+            lds_char* const meet = shared + (buffer ^ 1) * 2 * kTileBytes;
+            lds_char* const ends = meet + kRowWaves * 8 * 1024 + row_wave * 512;
+            float f = 1.0f, g = 1.0f;
+            barrier();
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+            for (int half = 0; half < 2; ++half) {
+                if (part == 1) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const f32x4 x = {r.o[d][4 * i] * inv, r.o[d][4 * i + 1] * inv, r.o[d][4 * i + 2] * inv, r.o[d][4 * i + 3] * inv};
-                *(lds_f16x4*)(own + in * kRowBytes + k_piece(in, 4 * d + i) * 16 + upper * 8) =
-                    __builtin_convertvector(x, f16x4);
+                    for (int i = 0; i < 8; ++i) {
+                        const int d = 2 * half + i / 4, e = i % 4 * 4;
+                        *(lds_f32x4*)(meet + ((row_wave * 8 + i) * 64 + lane) * 16) =
+                            f32x4{r.o[d][e], r.o[d][e + 1], r.o[d][e + 2], r.o[d][e + 3]};
+                    }
+                    if (half == 0) *(lds_f32x2*)(ends + lane * 8) = f32x2{r.top, sum};
+                }
+                barrier();
+                if (part == 0) {
+                    if (half == 0) {
+                        const f32x2 other = *(const lds_f32x2*)(ends + lane * 8);
+                        const float top = fmaxf(r.top, other[0]);
+                        f = r.top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.top - top);
+                        g = other[0] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(other[0] - top);
+                        sum = f * sum + g * other[1];
+                        r.top = top;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int d = 2 * half + i / 4, e = i % 4 * 4;
+                        const f32x4 z = *(const lds_f32x4*)(meet + ((row_wave * 8 + i) * 64 + lane) * 16);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) r.o[d][e + j] = f * r.o[d][e + j] + g * z[j];
+                    }
+                }
+                if (half == 0) barrier();
             }
+        }
+        if (part == 0) {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            lse = (r.top - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
+            const unsigned in = lane_again() & 31, upper = lane_again() >> 5;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 x = {r.o[d][4 * i] * inv, r.o[d][4 * i + 1] * inv, r.o[d][4 * i + 2] * inv, r.o[d][4 * i + 3] * inv};
+                    *(lds_f16x4*)(own + in * kRowBytes + k_piece(in, 4 * d + i) * 16 + upper * 8) =
+                        __builtin_convertvector(x, f16x4);
+                }
+        }
         stored = false;
         before = w;
         w = ahead;
@@ -323,18 +381,29 @@ extern "C" int apex_steps_prompt_attention(const void* q, int64_t q_token_stride
     a.G = divisor((unsigned)(Hq / Hkv));
     a.c = (scale < 0 ? -scale : scale) * kLog2e;
     a.negate = scale < 0;
-    constexpr int kWaves = 8, kRows = kWaves * kWaveRows;
-    const unsigned slots = (unsigned)((int64_t)T * a.G.d / kRows) + (unsigned)B;
     int units = 0;
     rc = compute_units(&units);
     if (rc != APEX_OK) return rc;
-    const unsigned items = slots * (unsigned)Hkv, groups = items < (unsigned)units ? items : (unsigned)units;
+    const int64_t rows = (int64_t)T * a.G.d;
+    // Parts pay where a prompt's own chain of tiles is what takes the time: few items,
+    // not too short, or about two to a unit if they are long.  32 over 8 heads, parts
+    // and none: one prompt of 256 tokens 11.1 us and 12.5, of 1024 24.9 and 32.8, of
+    // 2048 50 and 61; but of 100 9.4 and 9.2, of 4096 165 and 143, four of 512 tokens
+    // 25.6 and 22.5.
+    const int64_t parts_items = (rows / 128 + B) * Hkv, mean = T / B;
+    if (mean >= 256 && 4 * parts_items <= (mean >= 1024 ? 9 : 5) * (int64_t)units) {
+        const unsigned items = (unsigned)parts_items;
+        prompt_kernel<2><<<items, 64 * kWaves, 0, (hipStream_t)stream>>>(a, items / (unsigned)Hkv, items, 1);
+        return launched("prompt_attention");
+    }
+    const unsigned slots = (unsigned)(rows / 256) + (unsigned)B, items = slots * (unsigned)Hkv,
+                   groups = items < (unsigned)units ? items : (unsigned)units;
     // From eight items a work group on the sums are alike enough: 32768 tokens, 16
     // items, 8.42 ms with all of them dealt out and 8.54 with the cheapest two left.
     // Below, they are not: a chat batch of 16 prompts, 5 items, 89.5 us and 85.6.
     const double ratio = (double)items / groups;
     const unsigned rounds = ratio >= 8 ? (unsigned)((items + groups - 1) / groups) : ratio < 2 ? 1 : ratio < 4.5 ? 2 : ratio < 6.7 ? 4 : 6;
     const unsigned alone = items > rounds * groups ? items - rounds * groups : 0;
-    prompt_kernel<kWaves><<<groups + alone, 64 * kWaves, 0, (hipStream_t)stream>>>(a, slots, groups, rounds);
+    prompt_kernel<1><<<groups + alone, 64 * kWaves, 0, (hipStream_t)stream>>>(a, slots, groups, rounds);
     return launched("prompt_attention");
 }

@@ -256,6 +256,54 @@ def test_prompts_of_many_tiles(torch, steps, B, n, Hq, Hkv):
         check([(slice(0, sum(lens)), h, n, (out[:, h], ref[:, h], mag[:, h], most[:, h]))], got, lse, SCALE)
 
 
+@pytest.mark.parametrize("lens,Hq,Hkv", [([256], 1, 1), ([257], 4, 1), ([511], 3, 3), ([1100], 2, 2), ([2051], 4, 2), ([1, 0, 900], 8, 2),
+                                         ([64, 449], 16, 2), ([300, 320, 257], 6, 2), ([1500], 32, 4)])
+def test_prompts_whose_keys_two_waves_share(torch, steps, lens, Hq, Hkv):
+    """Few prompts of some length: every second 64 keys are another wave's."""
+    q, k, v, offsets = prompts(lens, Hq, Hkv, sum(lens) + Hq, pad=2)
+    k[64:128] *= np.float16(4)                  # some rows' largest weights in either's keys
+    got, lse = run_prompts(torch, steps, q, k, v, offsets, -SCALE)
+    assert (got[-2:] == 7).all() and (lse[-2:] == 7).all()
+    out, ref, mag, most = plain64(torch, *dev(torch, q, k, v), np.unique(offsets).tolist(), -SCALE)
+    for h in range(Hq):
+        check([(slice(0, sum(lens)), h, max(lens), (out[:, h], ref[:, h], mag[:, h], most[:, h]))], got, lse, SCALE)
+
+
+@pytest.mark.parametrize("dead", [range(0, 64), range(64, 128), range(0, 300), [i for i in range(500) if i // 64 % 2], range(0, 500)])
+def test_prompt_scores_of_minus_infinity_among_shared_keys(torch, steps, dead):
+    n, dead = 500, list(dead)
+    q, k, v, offsets = prompts([n], 2, 1, 19)
+    q[:, :, 0] = 1
+    k[:, :, 0] = 0
+    sees = np.ones(n, bool)
+    sees[dead] = False
+    k[dead, :, 0] = -np.inf
+    got, lse = run_prompts(torch, steps, q, k, v, offsets)
+    k[:, :, 0] = 0
+    for r in list(range(0, n, 7)) + [n - 1]:
+        keys = np.flatnonzero(sees[:r + 1])
+        for h in range(2):
+            if not len(keys):
+                assert (got[r, h] == 0).all() and np.isneginf(lse[r, h])
+                continue
+            one = O.attend(q[r:r + 1, h], k[keys, 0], v[keys, 0], SCALE, np.ones((1, len(keys)), bool))
+            check([(slice(0, 1), 0, len(keys), one)], got[r:r + 1, h:h + 1], lse[r:r + 1, h:h + 1], SCALE)
+
+
+@pytest.mark.parametrize("key", [70, 130, 299])
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+def test_prompt_later_values_do_not_count_where_keys_are_shared(torch, steps, key, value):
+    q, k, v, offsets = prompts([300], 4, 2, 20)
+    clean, _ = run_prompts(torch, steps, q, k, v, offsets)
+    v[key, 0, 5] = value
+    got, lse = run_prompts(torch, steps, q, k, v, offsets)
+    before, heads = np.arange(300) < key, slice(0, 2)
+    assert np.isclose(got[before], clean[before], rtol=2 ** -9, atol=2 ** -12).all()
+    assert np.isclose(got[:, 2:], clean[:, 2:], rtol=2 ** -9, atol=2 ** -12).all()
+    assert not np.isfinite(got[~before, heads, 5]).any()
+    assert np.isfinite(np.delete(got[:, heads], 5, -1)).all() and np.isfinite(lse).all()
+
+
 def test_attention_refuses_what_it_cannot_read(torch, steps):
     c = trees([20, 5], [3, 4], 4, 2, 40)
     a = device(torch, c)
