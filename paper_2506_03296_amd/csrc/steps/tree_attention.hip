@@ -1,5 +1,13 @@
 // tree_attention.hip -- attention of drafted tokens over a paged cache and each
 // other (include/apex_steps.h).
+//
+// A pair's rows, its G q-heads of all drafted tokens, read each K and V row once:
+// below some 200 rows the cache's bytes bound it, above the matrix cores.  32
+// requests of 4096-32768 tokens with 5-8 drafted ones, 32 over 8 heads, are 1.78 GB
+// and take 283 us: 6.3 TB/s, and 6.6 inside the stream of units; the rest is the
+// first loads (9 us with the launch), the ends of parts, and the join (6).  With
+// more rows the work of a unit bounds it (attend_tile.h): 16 requests of 8000 tokens,
+// 8, 16 and 32 drafted ones: 90, 110 and 137 us.
 #include "attend_tile.h"
 #include "steps_host.h"
 
@@ -12,9 +20,12 @@ constexpr int kSlabBytes = kBlockSize * kRowBytes;
 // A pair is one request, one kv-head and one tile of its rows.  Its keys are taken
 // in units of `keys` tokens: the cached ones, then one unit of the drafted ones.
 // All pairs' units lie in one row, each pair's behind kPairCost units that stand for
-// its start; the work groups that take part get equal shares of it.
+// its start (2, 4 and 6 were no better than 1); the work groups get equal shares of
+// it, one unit at least (one request of 500 tokens, shares of at least 1, 2 and 4:
+// 14.7, 15.2, 15.7 us).  A part of a pair leaves its sums in the workspace, for
+// join_kernel: a launch of its own, 4-6 us, where a count of the parts that have
+// come would have work groups wait for memory to be coherent.
 constexpr int kPairCost = 1;
-constexpr int kLeastShare = 1;
 
 struct TreeArgs {
     const char *q, *k_new, *v_new, *k_cache, *v_cache;
@@ -68,8 +79,9 @@ __device__ inline int request_cost(const Args& a, const Request& r)
     return r.nodes ? a.Hkv * r.tiles * (r.units + kPairCost) : 0;
 }
 
-// Eight waves: kRowWaves of them hold 32 rows each, kParts of them share a row tile's
-// keys, 32 kSub each of a unit.
+// Eight waves, one work group a compute unit: kRowWaves of them hold 32 rows each,
+// kParts of them share a row tile's keys, 32 kSub each of a unit.  (Two work groups of
+// four waves, for up to 32 rows: 335 us for 319.)
 constexpr int kWaves = 8;
 template <int kRowWaves_, int kSub_>
 struct Shape {
@@ -119,7 +131,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
     int total = __builtin_amdgcn_readlane(upto0, 63);
     for (int i = 64; i < a.B; i += 64)
         total += wave_sum(i + (int)lane < a.B ? request_cost(a, read_request<kTileRows, kKeys>(a, i + lane)) : 0);
-    const int active = min((int)gridDim.x, (total + kLeastShare - 1) / kLeastShare);
+    const int active = min((int)gridDim.x, total);
     if ((int)blockIdx.x >= active) return;
     const int share = uniform(total / active), longer = total - share * active;      // the first `longer` take one more
     const int begin = share * (int)blockIdx.x + min((int)blockIdx.x, longer);
@@ -444,7 +456,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
 }
 
 // Joins the parts of the pair that work group x's last part opens; 8 rows a work
-// group, 32 lanes a row.
+// group, 32 lanes a row.  Bound by its launch and two round trips, 3.4 us for small
+// tiles, 6 for 128 rows; 16 to 64 rows a work group made 52 us of a chat batch 53-57.
 __global__ __launch_bounds__(256) void join_kernel(TreeArgs a, int tile_rows)
 {
     const int4 job = a.joins[2 * blockIdx.x];
@@ -474,7 +487,11 @@ __global__ __launch_bounds__(256) void join_kernel(TreeArgs a, int tile_rows)
     if (a.lse && i == 0) a.lse[to] = (top - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// Shapes by the most rows of a pair.
+// Shapes by the most rows of a pair: the smallest that holds them, since waves of
+// rows that are not there still take their keys.  16 requests of 8000 tokens, 32 over
+// 8 heads, in shapes of 32, 64, 128 and 256: 32 rows 90, 105, 117, 166 us; 64 rows 110,
+// 124, 173; 128 rows 137, 189.  256 rows as one tile of 256 and as two of 128, on 8
+// requests of 4096 tokens: 76 and 79 us, 512 rows 125 and 132.
 using Shape32 = Shape<1, 1>;
 using Shape64 = Shape<2, 1>;
 using Shape128 = Shape<4, 2>;
