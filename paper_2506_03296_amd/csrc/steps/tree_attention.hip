@@ -120,7 +120,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
 
     const unsigned lane = threadIdx.x & 63, wave = (unsigned)uniform((int)(threadIdx.x >> 6));
     const unsigned half = lane >> 5;
-    const int row_wave = (int)wave % S::kRowWaves, part = (int)wave / S::kRowWaves;
+    const int row_wave = (int)wave / kParts, part = (int)wave % kParts;
     const int from = part * kWaveKeys;                   // this wave's keys of a unit
 
     // the share of this work group: [begin, end) of `total` units
@@ -302,29 +302,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
             }
         }
         lds_char* const kt = shared + (kOwn ? 0 : buffer * 2 * kBytes) + from * kRowBytes;
+        // a wave without rows or keys leaves its SIMD to the others
+        const int n = u < g.cached ? g.q.len - u * kKeys - from : g.q.nodes - from;      // the wave's keys
+        const bool works = n > 0 && (kOwn || row_wave * kWaveRows < g.q.nodes * (int)a.G.d - g.tile * kTileRows);
         f32x16 s[kSub];
-        r.scores(kt, s);
+        if (works) r.scores(kt, s);
         if (kOwn && more) {
             was_read();
             load(ahead, u_ahead, 0, false);
-        }
-        if (u < g.cached) {
-            uint64_t allow = 0;                          // the keys that are there
-#pragma unroll
-            for (int j = 0; j < S::kPartBlocks; ++j)
-                if (there >> j & 1) allow |= 0xffffull << (16 * j);
-            const int n = g.q.len - u * kKeys - from;
-            allow &= n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
-            if (allow != (kSub == 2 ? ~0ull : 0xffffffffull)) r.mask(s, allow);
-        } else {
-            const uint64_t nodes = from >= 64 ? 0 : (g.q.nodes >= 64 ? ~0ull : (1ull << g.q.nodes) - 1) >> from;
-            r.mask(s, tree >> (from & 63) & nodes);
         }
         if (kOwn) {
             if (more) arrived<kLoads>();                 // V; the next K is on its way
             else arrived<0>();
         }
-        r.take(s, c, kt + kBytes);
+        if (works) {
+            uint64_t allow = 0;                          // the keys that are there
+            if (u < g.cached) {
+#pragma unroll
+                for (int j = 0; j < S::kPartBlocks; ++j)
+                    if (there >> j & 1) allow |= 0xffffull << (16 * j);
+                allow &= n >= 64 ? ~0ull : (1ull << n) - 1;
+                if (allow != (kSub == 2 ? ~0ull : 0xffffffffull)) r.mask(s, allow);
+            } else {
+                r.mask(s, tree >> (from & 63) & (n >= 64 ? ~0ull : (1ull << n) - 1));
+            }
+            r.take(s, c, kt + kBytes);
+        }
         if (kOwn && !last) {
             was_read();
             load(ahead, u_ahead, 0, true);
@@ -380,13 +383,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
             sum = 0.0f;
 #pragma unroll
             for (int w = 0; w < kParts; ++w) {
-                f[w] = merge_top[w * S::kRowWaves + row_wave][lane & 31];
+                f[w] = merge_top[row_wave * kParts + w][lane & 31];
                 top = fmaxf(top, f[w]);
             }
 #pragma unroll
             for (int w = 0; w < kParts; ++w) {
                 f[w] = f[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(f[w] - top);
-                sum = __builtin_fmaf(f[w], merge_sum[w * S::kRowWaves + row_wave][lane & 31], sum);
+                sum = __builtin_fmaf(f[w], merge_sum[row_wave * kParts + w][lane & 31], sum);
             }
         }
         const unsigned row = row_of(g), G = out->G.d, node = divide(row, out->G);
@@ -416,7 +419,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
                     y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int w = 0; w < kParts; ++w) {
-                        const f32x4 z = *(const lds_f32x4*)(meet + (((w * S::kRowWaves + row_wave) * kQuads + i) * 64 + lane) * 16);
+                        const f32x4 z = *(const lds_f32x4*)(meet + (((row_wave * kParts + w) * kQuads + i) * 64 + lane) * 16);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) y[j] = __builtin_fmaf(f[w], z[j], y[j]);
                     }

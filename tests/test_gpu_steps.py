@@ -170,6 +170,39 @@ def test_prompt_out_of_a_fused_projection(torch, steps):
     assert got.all()
 
 
+@pytest.mark.parametrize("stride", [(1 << 23) - 8, (1 << 23) + 8])
+@pytest.mark.parametrize("lens", [[300], [100, 130, 69]])
+def test_prompt_rows_far_apart(torch, steps, lens, stride):
+    """Tokens 16 MiB apart: a tile's rows span 2^30 bytes and more, the batch 2^32."""
+    T, Hq, Hkv = sum(lens), 4, 2
+    q, k, v, offsets = prompts(lens, Hq, Hkv, T + stride % 16)
+    base = torch.empty(T * stride, dtype=torch.float16, device="cuda")
+    views, at = [], 0
+    for x in (q, k, v):
+        view = base.as_strided(x.shape, (stride, D, 1), at)
+        view.copy_(dev(torch, x))
+        views.append(view)
+        at += x.shape[1] * D
+    lse = torch.empty((T, Hq), dtype=torch.float32, device="cuda")
+    out = steps.prompt_attention(*views, dev(torch, offsets), SCALE, lse_out=lse)
+    assert check(O.prompt(q, k, v, offsets, SCALE), out.cpu().numpy(), lse.cpu().numpy(), SCALE).all()
+
+
+def test_tree_of_rows_far_apart(torch, steps):
+    c = trees([70, 0, 300], [40, 64, 3], 4, 2, 41)
+    args = list(device(torch, c))
+    T, stride = c["q"].shape[0], (1 << 25) + 8
+    base, at = torch.empty(T * stride, dtype=torch.float16, device="cuda"), 0
+    for i in range(3):
+        x = args[i]
+        args[i] = base.as_strided(x.shape, (stride, D, 1), at)
+        args[i].copy_(x)
+        at += x.shape[1] * D
+    lse = torch.empty((T, 4), dtype=torch.float32, device="cuda")
+    out = steps.tree_attention(*args, SCALE, lse_out=lse)
+    check(oracle(c), out.cpu().numpy(), lse.cpu().numpy(), SCALE)
+
+
 @pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
 @pytest.mark.parametrize("which", ["k", "v"])
 def test_prompt_later_tokens_do_not_count(torch, steps, which, value):
@@ -353,6 +386,24 @@ def test_prompt_captured_and_replayed(torch, steps):
     graph.replay()
     torch.cuda.synchronize()
     assert check(O.prompt(q, k, v, [0, 5, 100, 191], SCALE), out.cpu().numpy(), lse.cpu().numpy(), SCALE).all()
+
+
+def test_prompts_whose_keys_two_waves_share_replayed_with_other_lengths(torch, steps):
+    q, k, v, offsets = prompts([600, 100], 4, 2, 21)
+    dq, dk, dv, do = dev(torch, q, k, v, offsets)
+    out = torch.zeros_like(dq)
+    lse = torch.zeros(q.shape[:2], dtype=torch.float32, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        steps.prompt_attention(dq, dk, dv, do, SCALE, out=out, lse_out=lse)
+    for other in ([0, 600, 700], [0, 0, 700], [0, 700, 700], [0, 1, 129], [0, 64, 640]):
+        do.copy_(torch.tensor(other, dtype=torch.int32))
+        out.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.cpu().numpy()
+        rows = check(O.prompt(q, k, v, other, SCALE), got, lse.cpu().numpy(), SCALE)
+        assert rows[:other[-1]].all() and (got[other[-1]:] == 7).all()
 
 
 # --- trees -----------------------------------------------------------------------
