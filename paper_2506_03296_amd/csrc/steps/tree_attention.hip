@@ -92,7 +92,10 @@ struct Shape {
     static constexpr int kBytes = kKeys * kRowBytes;             // of a unit's K or V
     // A wave brings the keys that it takes and no others, into one buffer, each half
     // of which it fills again as soon as it has read it (kOwn), or the work group's
-    // waves bring a unit together, into one of two buffers.
+    // waves bring a unit together, into one of two buffers.  64 rows with a copy of
+    // the keys for each of the two waves that take them, and no barrier: 95 us for the
+    // 81 of 16 full trees over 32 heads; K brought one and a half units ahead, with a
+    // second barrier a unit: 88.
     static constexpr bool kOwn = kRowWaves == 1;
     static constexpr int kBuffers = kOwn ? 1 : 2, kLds = 2 * kBuffers * kBytes;
     static constexpr int kLoads = kKeys / (4 * kWaves);          // of K, and of V, by which a wave brings its share of a unit
@@ -490,8 +493,8 @@ __global__ __launch_bounds__(256) void join_kernel(TreeArgs a, int tile_rows)
     if (a.lse && i == 0) a.lse[to] = (top - kBias + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// Shapes by the most rows of a pair: the smallest that holds them, since waves of
-// rows that are not there still take their keys.  16 requests of 8000 tokens, 32 over
+// Shapes by the most rows of a pair: the smallest that holds them, whose waves share
+// the keys of a row among the most of them.  16 requests of 8000 tokens, 32 over
 // 8 heads, in shapes of 32, 64, 128 and 256: 32 rows 90, 105, 117, 166 us; 64 rows 110,
 // 124, 173; 128 rows 137, 189.  256 rows as one tile of 256 and as two of 128, on 8
 // requests of 4096 tokens: 76 and 79 us, 512 rows 125 and 132.
