@@ -301,11 +301,12 @@ struct Rows {
 
     // The weights of a unit's scores and their products with V: V's operands come
     // while weights are made, and the weights of 32 keys are made while the matrix
-    // cores work on the 32 before them.
-    __device__ void take(const f32x16 (&s)[kSub], float c, const lds_char* v)
+    // cores work on the 32 before them.  `half`: none of the second 32 is seen.
+    __device__ void take(const f32x16 (&s)[kSub], float c, const lds_char* v, bool half = false)
     {
 #pragma unroll
         for (int u = 0; u < kSub; ++u) {
+            if (u && half) break;
             f16x8 a[2][4];
             read_v(v, u, a);
             if (u == 0) raise(s, c);

@@ -3,7 +3,9 @@
 // An item is one kv-head of one request and a tile of its rows, position by position
 // the G q-heads of each: a work group walks over the keys up to its last row's in
 // tiles of 64, in the one pass of attend_tile.h, and masks the tiles that its waves'
-// diagonals cross.  A wave leaves out the tiles behind its own last row.
+// diagonals cross.  A wave leaves out the tiles behind its own last row, and of its
+// last tile the weights of a second half that it does not see (batches 0-2 % faster;
+// leaving out its scores too needs a second copy of the loop, which spills).
 //
 // The matrix cores bound it from some 500 tokens on: 32768 tokens of 32 over 8 heads
 // are 8.8 TFLOP and take 8.3 to 8.7 ms, 1010-1060 TFLOP/s of the 1200 of a large
@@ -258,13 +260,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
             bring(t);
             const lds_char* kt = shared + buffer * 2 * kTileBytes + part * kPartKeys * kRowBytes;
             const int own_t = t * kParts + (int)part;       // the wave's keys, in 64s
-            f32x16 s[2];
-            r.scores(kt, s);
-            if ((own_t + 1) * kPartKeys > wave_lo + 1) {
-                const int seen = pos - own_t * kPartKeys + 1;       // of them, those up to the row's own
-                r.mask(s, seen >= 64 ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
+            if (kParts == 1 || own_t * kPartKeys <= wave_hi) {
+                f32x16 s[2];
+                r.scores(kt, s);
+                if ((own_t + 1) * kPartKeys > wave_lo + 1) {
+                    const int seen = pos - own_t * kPartKeys + 1;       // of them, those up to the row's own
+                    r.mask(s, seen >= 64 ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
+                }
+                r.take(s, a.c, kt + kTileBytes, wave_hi < own_t * kPartKeys + 32);
             }
-            r.take(s, a.c, kt + kTileBytes);
             buffer ^= 1;
             if (t + 1 < tiles) {
                 arrived<0>();
