@@ -8,7 +8,7 @@
 // leaving out its scores too needs a second copy of the loop, which spills).
 //
 // The matrix cores bound it from some 500 tokens on: 32768 tokens of 32 over 8 heads
-// are 8.8 TFLOP and take 8.3 to 8.7 ms, 1010-1060 TFLOP/s of the 1200 of a large
+// are 8.8 TFLOP and take 8.3 to 9.0 ms, 975-1060 TFLOP/s of the 1200 of a large
 // library product; what holds a wave back is said in attend_tile.h.  One prompt has
 // few items and its longest bounds it: 1024 tokens 25 us, 4096 143.
 //
