@@ -163,7 +163,7 @@ struct ReleaseArgs {
 };
 
 constexpr int kReleaseThreads = 1024;
-constexpr int kEntries = 8;      // of a thread at a time
+constexpr int kEntries = 8;      // of a thread at a time (16 and 24: 25.9 and 34.0 us a call for 24 on 25 948 blocks)
 
 // One work group: where an id goes depends on how many of those before it count.
 // It takes 8192 entries of the rows at a time, neighbouring lanes neighbouring
