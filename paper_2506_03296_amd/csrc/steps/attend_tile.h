@@ -172,11 +172,11 @@ struct Rows {
         for (int j = 0; j < 8; ++j) q[j] = *(const lds_f16x8*)(rows + row * kRowBytes + k_piece(row, 2 * j + half) * 16);
     }
 
-    // A negative scale is taken as its magnitude, with q's sign turned.
-    __device__ void negate()
+    // The scale's sign, see QScale.
+    __device__ void times(_Float16 sign)
     {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = __builtin_bit_cast(f16x8, __builtin_bit_cast(u32x4, q[j]) ^ 0x80008000u);
+        for (int j = 0; j < 8; ++j) q[j] *= sign;
     }
 
     __device__ void clear()
@@ -299,6 +299,21 @@ struct Rows {
             for (int t = 0; t < 4; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[w][t], p[w], o[t], 0, 0, 0);
     }
 
+    // False if a unit's values hold an infinity or a NaN.  A masked key has the weight
+    // 0, but 0 x NaN is NaN: where rows differ in what they see, a row's last 64 keys at
+    // most, a unit that is not finite is taken key by key (take_key).  Everywhere else
+    // an infinity or a NaN is the rows' own.
+    __device__ static bool finite(const lds_char* v)
+    {
+        const unsigned lane = lane_again();
+        const f16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+        f16x8 x = zero;
+#pragma unroll
+        for (int i = 0; i < 8 * kSub; ++i) x = __builtin_elementwise_fma(*(const lds_f16x8*)(v + (i * 64 + lane) * 16), zero, x);
+        const u32x4 bits = __builtin_bit_cast(u32x4, x);        // 0 x finite + 0 is +0
+        return !__any((bits[0] | bits[1] | bits[2] | bits[3]) != 0);
+    }
+
     // The weights of a unit's scores and their products with V: V's operands come
     // while weights are made, and the weights of 32 keys are made while the matrix
     // cores work on the 32 before them.  `half`: none of the second 32 is seen.
@@ -314,19 +329,6 @@ struct Rows {
             weights(s[u], c, p);
             add(a, p);
         }
-    }
-
-    // True if some sum of the wave's is an infinity or a NaN.  That need not be the
-    // rows' own: a masked key has the weight 0, but 0 x NaN is NaN.  The wave then
-    // clears its sums and takes its keys anew, one by one.
-    __device__ bool spoiled() const
-    {
-        float x = 0.0f;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x += o[t][i];
-        return __any(!(fabsf(x) < INFINITY));
     }
 
     // One key, by its rows in global memory (this kv-head's), for the queries that see it.
@@ -360,6 +362,18 @@ struct Rows {
             }
     }
 };
+
+// A scale as the kernels take it: q times `sign`, -1, 1 or 0, and c = |scale| log2 e.  For
+// a scale of 0 the zeros go into q, and c is 1: a masked score, -inf, stays what it is.
+struct QScale {
+    float c;
+    _Float16 sign;
+};
+
+inline QScale q_scale(float scale)
+{
+    return {scale == 0.0f ? 1.0f : (scale < 0.0f ? -scale : scale) * kLog2e, (_Float16)(scale == 0.0f ? 0 : scale < 0.0f ? -1 : 1)};
+}
 
 // Division by a number that the host knows, of numbers below 2^31: with s the
 // least power of two that is not below d, floor((n m / 2^32 + n) / 2^s) for

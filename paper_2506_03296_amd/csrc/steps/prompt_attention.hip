@@ -34,8 +34,7 @@ struct PromptArgs {
     int64_t q_stride, kv_stride;   // bytes between tokens
     int B, T, Hq;
     Divisor Hkv, G;
-    float c;                       // |scale| log2 e
-    bool negate;
+    QScale scale;
 };
 
 // One request's rows in the packed arrays, cut to [0, T].
@@ -253,7 +252,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
                 load_q(ahead);
             }
         };
-        if (a.negate) r.negate();
+        if (a.scale.sign != (_Float16)1) r.times(a.scale.sign);
         r.clear();
         int t = 0;
         for (; t < own_tiles; ++t) {
@@ -263,11 +262,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
             if (kParts == 1 || own_t * kPartKeys <= wave_hi) {
                 f32x16 s[2];
                 r.scores(kt, s);
+                int finite = 1;
                 if ((own_t + 1) * kPartKeys > wave_lo + 1) {
                     const int seen = pos - own_t * kPartKeys + 1;       // of them, those up to the row's own
                     r.mask(s, seen >= 64 ? ~0ull : seen <= 0 ? 0ull : (1ull << seen) - 1);
+                    finite = r.finite(kt + kTileBytes);
                 }
-                r.take(s, a.c, kt + kTileBytes, wave_hi < own_t * kPartKeys + 32);
+                finite = uniform(finite);
+                if (__builtin_expect(finite, 1)) r.take(s, a.scale.c, kt + kTileBytes, wave_hi < own_t * kPartKeys + 32);
+                asm volatile("" : "+s"(finite));     // one branch, of both, spills the sums
+                if (__builtin_expect(!finite, 0)) {
+#pragma nounroll
+                    for (int key = own_t * kPartKeys; key <= min(own_t * kPartKeys + kPartKeys - 1, wave_hi); ++key) {
+                        const int64_t at = (int64_t)(w.first + key) * a.kv_stride + w.head * kRowBytes;
+                        r.take_key(a.k + at, a.v + at, a.scale.c, key <= pos);
+                    }
+                }
             }
             buffer ^= 1;
             if (t + 1 < tiles) {
@@ -281,16 +291,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
             if (t + 1 < tiles) {
                 arrived<0>();
                 barrier();
-            }
-        }
-        if (__builtin_expect(r.spoiled(), 0)) {
-            r.clear();
-#pragma nounroll
-            for (int key = 0; key <= wave_hi; ++key) {
-                if (kParts == 2 && (unsigned)key / kPartKeys % 2 != part) key += kPartKeys;
-                if (key > wave_hi) break;
-                const int64_t at = (int64_t)(w.first + key) * a.kv_stride + w.head * kRowBytes;
-                r.take_key(a.k + at, a.v + at, a.c, key <= pos);
             }
         }
         if (more) {
@@ -399,8 +399,7 @@ extern "C" int apex_steps_prompt_attention(const void* q, int64_t q_token_stride
     a.Hq = Hq;
     a.Hkv = divisor((unsigned)Hkv);
     a.G = divisor((unsigned)(Hq / Hkv));
-    a.c = (scale < 0 ? -scale : scale) * kLog2e;
-    a.negate = scale < 0;
+    a.scale = q_scale(scale);
     int units = 0;
     rc = compute_units(&units);
     if (rc != APEX_OK) return rc;

@@ -40,8 +40,7 @@ struct TreeArgs {
     int64_t table_stride, num_blocks;
     int B, T, max_nodes, Hq, Hkv;
     Divisor G;
-    float c;
-    bool negate;
+    QScale scale;
 };
 
 // The kernel's arguments, read again: what only the ends of a part need does not
@@ -283,8 +282,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
     unsigned there = present(), buffer = 0;
     load(g, g.lo, 0, false);
     load(g, g.lo, 0, true);
-    if (a.negate) r.negate();
-    const float c = a.c;
+    if (a.scale.sign != (_Float16)1) r.times(a.scale.sign);
+    const float c = a.scale.c;
     for (int u = g.lo;;) {
         // the unit that is brought while this one is worked on: the part's next, or
         // the first of the work group's next part
@@ -319,6 +318,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
             else arrived<0>();
         }
         if (works) {
+            int finite = 1;
             uint64_t allow = 0;                          // the keys that are there
             if (u < g.cached) {
 #pragma unroll
@@ -328,8 +328,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
                 if (allow != (kSub == 2 ? ~0ull : 0xffffffffull)) r.mask(s, allow);
             } else {
                 r.mask(s, tree >> (from & 63) & (n >= 64 ? ~0ull : (1ull << n) - 1));
+                finite = r.finite(kt + kBytes);
             }
-            r.take(s, c, kt + kBytes);
+            finite = uniform(finite);
+            if (__builtin_expect(finite, 1)) r.take(s, c, kt + kBytes);
+            asm volatile("" : "+s"(finite));     // one branch, of both, spills the sums
+            if (__builtin_expect(!finite, 0)) {
+                const Arguments f = arguments();
+#pragma nounroll
+                for (int i = 0; i < min(n, kWaveKeys); ++i) {
+                    const int64_t at = (int64_t)(g.q.first + from + i) * f->new_stride + g.kv_head * kRowBytes;
+                    r.take_key(f->k_new + at, f->v_new + at, c, tree >> (from + i) & 1);
+                }
+            }
         }
         if (kOwn && !last) {
             was_read();
@@ -344,31 +355,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
 
         // the part's end
         const Arguments out = arguments();
-        if (__builtin_expect(r.spoiled(), 0)) {
-            r.clear();
-            const int32_t* row = out->table + (int64_t)g.b * out->table_stride;
-#pragma nounroll
-            for (int i = 0; i < (g.hi - g.lo) * kWaveKeys; ++i) {
-                const int v = g.lo + i / kWaveKeys, key = from + i % kWaveKeys;
-                const char *k_row = (const char*)kZeros, *v_row = k_row;
-                bool is_there = false;
-                if (v < g.cached) {
-                    const int id = v * kKeys + key < g.q.len ? id_of(g, row, v, key) : -1;
-                    if ((unsigned)id < num_blocks) {
-                        const int64_t to = (int64_t)id * block_bytes + (int64_t)g.kv_head * kSlabBytes + key % kBlockSize * kRowBytes;
-                        k_row = out->k_cache + to;
-                        v_row = out->v_cache + to;
-                        is_there = true;
-                    }
-                } else if (key < g.q.nodes) {
-                    const int64_t to = (int64_t)(g.q.first + key) * out->new_stride + g.kv_head * kRowBytes;
-                    k_row = out->k_new + to;
-                    v_row = out->v_new + to;
-                    is_there = true;
-                }
-                r.take_key(k_row, v_row, c, is_there && (v < g.cached || (tree >> (key & 63) & 1)));
-            }
-        }
         if (more) rows(ahead);                           // on their way while the parts meet
 
         // the parts' sums together, each wave of a tile some of the dims
@@ -453,7 +439,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
             barrier();                                   // all have met
             load(ahead, u_ahead, 0, true);
         }
-        if (a.negate) r.negate();
+        if (a.scale.sign != (_Float16)1) r.times(a.scale.sign);
         r.clear();
         g = ahead;
         u = g.lo;
@@ -638,8 +624,7 @@ int apex_steps_tree_attention(const void* q, int64_t q_token_stride, const void*
     a.Hq = Hq;
     a.Hkv = Hkv;
     a.G = divisor((unsigned)G);
-    a.c = (scale < 0 ? -scale : scale) * kLog2e;
-    a.negate = scale < 0;
+    a.scale = q_scale(scale);
     const hipStream_t on = (hipStream_t)stream;
     const auto kernel = rows == 32 ? tree_kernel<Shape32> : rows == 64 ? tree_kernel<Shape64>
                         : rows == 128 ? tree_kernel<Shape128> : tree_kernel<Shape256>;
