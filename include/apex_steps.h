@@ -28,8 +28,11 @@
  * aligned, the other arrays to their element.  q-head h attends kv-head
  * h / (Hq / Hkv); any Hq that is a multiple of Hkv is supported.  lse_out (fp32
  * [T][Hq], may be NULL) is the natural-log log-sum-exp of the scaled logits.
- * Scores, softmax and sums are fp32, the softmax's weights enter the product
- * with V as fp16.  A row that attends nothing gives zeros and -inf.  What a row
+ * Scores, softmax and sums are fp32.  The softmax's weights enter the product with
+ * V as fp16: of the drafted tokens' attention in two parts, as the decode
+ * attention's do, so that what is left is the output's own rounding; of the prompts'
+ * in one, off by up to 2^-11 of a weight (and by 2^-36 of a row's largest).  A row
+ * that attends nothing gives zeros and -inf.  What a row
  * does not attend has no influence on it, infinities and NaNs among it.
  * Supported: d = 128, B <= 2^22, Hq <= 2^16, (T + 256) * Hq < 2^30, B * Hkv + (T + 32) *
  * Hq / 32 < 2^30, strides < 2^31; block_size 16 for the attention, any for extend and release; anything else returns

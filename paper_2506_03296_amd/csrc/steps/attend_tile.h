@@ -13,12 +13,19 @@
 // keys of a step; V^T is read in that naming too, so they stay where they are.
 //
 // Rounding: scores, maxima, sums and O are fp32.  The weights enter the second
-// product as fp16 (half a step: up to 2^-11 of a weight, at random), which the output's
-// own rounding to fp16 matches.  They are 2^kBias times what the softmax defines, or
-// more, so that this holds down to 2^-25 of the row's largest weight; what is
-// smaller lies among fp16's subnormal numbers and is off by up to 2^-36 of the largest
-// (2^-(25 + kBias)).  Against 64 bits the results are off by 2.3e-4 to 2.9e-4 relative,
-// those of products with fp32 weights by 1.9e-4 to 2.1e-4.
+// product as fp16, 2^kBias times what the softmax defines or more.
+//   Prompts: one part, off by up to 2^-11 of a weight, at random, which the output's own
+//   rounding to fp16 matches; below 2^-25 of the row's largest weight, among fp16's
+//   subnormal numbers, by up to 2^-36 of the largest (2^-(25 + kBias)).  Against 64
+//   bits the results are off by 2.3e-4 to 2.6e-4 relative, with fp32 weights 1.8e-4 to
+//   2.1e-4.  A second part is half as many products again where products are what
+//   takes the time: 8.2 ms would be 11.1 for 32768 tokens, 84 us 100 for a chat batch.
+//   Trees (kFine): two parts, as the decode attention has them, since a drafted token's
+//   row is to be what a decode step would give; off by up to 2^-21 of a weight, and by
+//   2^-36 of the largest.  What is left is the output's own rounding.  Where the cache's
+//   bytes are what takes the time it is free: up to 32 rows a pair 0-2 % (32 long
+//   contexts 284 us either way), 64 rows 1-3 %; 128 rows cost 7-14 % (a chat batch 51.8
+//   us and 56.1), 256 rows 9-20 %.
 //
 // What bounds it: the instructions of a wave.  64 keys are 32 matrix products, 1024
 // cycles, and the conversions, maxima and exponentials of 2048 weights, which depend
@@ -148,8 +155,9 @@ __device__ inline void barrier()
 
 __device__ inline unsigned lds_address(const lds_char* p) { return (unsigned)(uintptr_t)p; }
 
-// One wave's 32 rows; kSub tiles of 32 keys are taken at a time.
-template <int kSub>
+// One wave's 32 rows; kSub tiles of 32 keys are taken at a time.  kFine: the weights go
+// in as two fp16 parts.
+template <int kSub, bool kFine>
 struct Rows {
     f16x8 q[8];          // lane n and n + 32: row n, dims 16 j + 8 (lane / 32) + 0..7 in q[j]
     f32x16 o[4];         // O^T, dims 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4 in o[t][i], times 2^kBias
@@ -242,7 +250,8 @@ struct Rows {
     }
 
     // Weights of 32 keys' scores, as P^T's operands: keys 16 w + 4 half + 0..3 and + 8 in p[w].
-    __device__ void weights(const f32x16& s, float c, f16x8* p)
+    // kFine: p rounds towards 0, and `rest` has what is left.
+    __device__ void weights(const f32x16& s, float c, f16x8* p, f16x8* rest)
     {
         // a row that has seen no score yet keeps M = -inf: 2^(-inf - 0) = 0
         const float base = (top == -INFINITY ? 0.0f : top) - kBias;
@@ -256,7 +265,14 @@ struct Rows {
                 e[1] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[8 * w + j + 1], c, -base));
                 part[0] += e[0];
                 part[1] += e[1];
-                const f16x2 h = __builtin_convertvector(e, f16x2);
+                f16x2 h = __builtin_convertvector(e, f16x2);
+                if (kFine) {
+                    h = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(e[0], e[1]));
+                    const f32x2 d = {__builtin_fmaf((float)h[0], -1.0f, e[0]), __builtin_fmaf((float)h[1], -1.0f, e[1])};
+                    const f16x2 l = __builtin_convertvector(d, f16x2);
+                    rest[w][j] = l[0];
+                    rest[w][j + 1] = l[1];
+                }
                 p[w][j] = h[0];
                 p[w][j + 1] = h[1];
             }
@@ -329,9 +345,10 @@ struct Rows {
             f16x8 a[2][4];
             read_v(v, u, a);
             if (u == 0) raise(s, c);
-            f16x8 p[2];
-            weights(s[u], c, p);
+            f16x8 p[2], rest[2];
+            weights(s[u], c, p, rest);
             add(a, p);
+            if (kFine) add(a, rest);
         }
     }
 

@@ -181,7 +181,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prompt_kernel(PromptArgs a, un
             load_to_lds(v, to + kTileBytes + j * 4 * kWaves * kRowBytes);
         }
     };
-    Rows<2> r;
+    Rows<2, false> r;
     const auto row0 = [&](const Work& w) { return (unsigned)w.tile * kRows + row_wave * kWaveRows; };      // the wave's first row
     // The wave's rows of q and its results share a piece of LDS: rows of 256 bytes, laid out as K's.
     lds_char* const own = shared + 4 * kTileBytes + row_wave * kWaveRows * kRowBytes;

@@ -260,7 +260,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void tree_kernel(TreeArgs a)
             if ((unsigned)part_ids[j] < num_blocks) bits |= 1u << j;
         return bits;
     };
-    Rows<kSub> r;
+    Rows<kSub, true> r;
     uint64_t tree;                                       // the drafted tokens that the lane's rows see
     const auto row_of = [&](const Segment& g) {
         return (unsigned)(g.tile * kTileRows + row_wave * kWaveRows) + (lane_again() & 31);

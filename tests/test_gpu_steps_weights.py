@@ -60,3 +60,32 @@ def test_tree_weights_far_below_the_largest(torch, steps, nodes, gap, size):  # 
         tol = tolerance(L, 1.0, most, mag, out, size * L, np.exp(lse - most), 2.0 ** -11)
         diff = np.abs(got[at, h].astype(np.float64) - out)
         assert np.all(diff <= tol), (h, float((diff / tol).max()))
+
+
+# Trees take the weights in two parts.  Rows here attend few keys, whose scores are
+# exact (one product a row), so that little but the weights and the output's rounding is
+# left: the score times c = log2 e and the exponential's argument, 2^-24 of up to 8 log2 e
+# each and c's own rounding as much, 3 x 12 x 2^-24 x ln 2 of a weight; the exponential
+# and the factors that join parts 4 x 2^-22; the weight's parts 2^-21; sums of n numbers
+# (n + 8) x 2^-24.  Numerator and denominator: twice that.
+@pytest.mark.parametrize("negative", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,nodes", [(4, 1, [8, 3, 5]), (4, 2, [1, 7, 8]), (4, 1, [16, 9, 12]), (4, 1, [32, 17, 20]), (4, 1, [64, 33, 50]),
+                                          (8, 1, [64, 40, 64])])
+def test_tree_outputs_are_the_nearest_but_for_fp32(torch, steps, Hq, Hkv, nodes, negative):  # noqa: F811
+    rng = np.random.default_rng(Hq + nodes[0])
+    c = trees([20, 0, 3], nodes, Hq, Hkv, 63 + nodes[0])
+    c["q"][:] = 0
+    c["q"][:, :, 0] = rng.choice([0.5, 1, 2], c["q"].shape[:2])
+    for k in (c["k"], c["kc"]):
+        k[..., 0] = rng.uniform(-4, 4, k.shape[:-1])
+    for v in (c["v"], c["vc"]):
+        v[:] = 4 * v
+    scale = -1.0 if negative else 1.0
+    got, _ = run_trees(torch, steps, c, scale)
+    for at, h, n, (out, _, mag, _) in oracle(c, scale):
+        rel = 2 * (36 * 2.0 ** -24 * np.log(2) + 4 * 2.0 ** -22 + 2.0 ** -21 + (n + 8) * 2.0 ** -24)
+        with np.errstate(over="ignore"):
+            step = np.spacing(np.abs(out).astype(np.float16)).astype(np.float64)
+        tol = rel * mag + FLOOR * n * 16 + step / 2
+        diff = np.abs(got[at, h].astype(np.float64) - out)
+        assert np.all(diff <= tol), (h, n, float((diff / tol).max()), float((diff - step / 2).max()))
