@@ -111,7 +111,15 @@ def release_workspace():
 
 def tree_workspace_bytes(max_nodes, Hq, Hkv):
     """Bytes of a tree attention's workspace on the current device (0: bad shapes)."""
+    for x, name in ((max_nodes, "max_nodes"), (Hq, "Hq"), (Hkv, "Hkv")):
+        _c_int(x, name)
     return int(load_library().apex_steps_tree_workspace_bytes(max_nodes, Hq, Hkv))
+
+
+def _c_int(x, name):
+    """An error unless x fits a C int, which ctypes would cut it to."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} = {x} does not fit 32 bits")
 
 
 def _want(t, name, dtype, shape, device, index):
@@ -164,10 +172,12 @@ def _rows(t, name, heads, device, index):
     return s[0]
 
 
-def _blocks(context_lens, lens, name, block_table, free_blocks, free_state):
+def _blocks(context_lens, lens, name, block_table, free_blocks, free_state, block_size):
     """Checks common to extend and release: (device, index, B, entries per table row, blocks)."""
     dev, index = _gpu(block_table, "block_table")
     B, nb, shape = context_lens.numel(), free_blocks.numel(), block_table.shape
+    _c_int(B, "B")
+    _c_int(block_size, "block_size")
     if not (len(shape) == 2 and shape[0] == B
             and _words((block_table, context_lens, lens, free_blocks, free_state), (shape, (B,), (B,), (nb,), (2,)), index)):
         i32 = _torch().int32
@@ -202,7 +212,8 @@ def extend(context_lens, new_lens, block_table, free_blocks, free_state, T, bloc
     if given, else a new one).  ``block_table`` and ``free_state`` are updated in
     place; a request whose total_lens is not context_lens + new_lens was refused."""
     torch = _torch()
-    dev, index, B, stride, nb = _blocks(context_lens, new_lens, "new_lens", block_table, free_blocks, free_state)
+    _c_int(T, "T")
+    dev, index, B, stride, nb = _blocks(context_lens, new_lens, "new_lens", block_table, free_blocks, free_state, block_size)
     if plan is None:
         if T < 0:
             raise ValueError(f"T = {T} is negative")
@@ -228,7 +239,7 @@ def release(context_lens, keep_lens, block_table, free_blocks, free_state, block
     """apex_steps_release over torch tensors: the blocks that keep_lens[b] of a
     request's context_lens[b] tokens do not need go back to ``free_blocks``.
     ``block_table``, ``free_blocks`` and ``free_state`` are updated in place."""
-    _, index, B, stride, nb = _blocks(context_lens, keep_lens, "keep_lens", block_table, free_blocks, free_state)
+    _, index, B, stride, nb = _blocks(context_lens, keep_lens, "keep_lens", block_table, free_blocks, free_state, block_size)
     _call("apex_steps_release", index, context_lens.data_ptr(), keep_lens.data_ptr(), block_table.data_ptr(), stride,
           free_blocks.data_ptr(), free_state.data_ptr(), B, block_size, nb, _raw_stream(stream, index))
 
@@ -318,6 +329,7 @@ def tree_attention(q, k_new, v_new, token_offsets, tree_mask, k_cache, v_cache, 
     is an optional uint8 tensor of tree_workspace_bytes(max_nodes, Hq, Hkv) bytes;
     calls that can overlap, and a captured graph, need one of their own."""
     torch = _torch()
+    _c_int(max_nodes, "max_nodes")
     index, B, T, Hq, Hkv, qs, ks = _packed(q, k_new, v_new, ("k_new", "v_new"), token_offsets)
     dev = q.device
     _want(tree_mask, "tree_mask", torch.int64, (T,), dev, index)
