@@ -28,10 +28,10 @@
 //   us and 56.1), 256 rows 9-20 %.
 //
 // What bounds it: the instructions of a wave.  64 keys are 32 matrix products, 1024
-// cycles, and the conversions, maxima and exponentials of 2048 weights, which depend
+// cycles (48 with weights in two parts), and the conversions, maxima and exponentials of 2048 weights, which depend
 // on the first half of the products and feed the second: a wave's own do not overlap
 // much, so two waves of a SIMD have to fill each other's gaps.  Eight waves take a
-// tile in 1.7 to 2.0 us, the matrix cores busy 48 % of it.  LDS has no bank conflicts.
+// tile in 1.7 to 2.0 us, the matrix cores busy 53 % of it.  LDS has next to no bank conflicts.
 // Other orders were measured and left: the products of the next 32 keys between the
 // weights of these (5-10 % slower), half of the waves a phase behind the others
 // (1-3 %), priorities around the products (0-1.5 %), two row tiles a wave with one

@@ -3,17 +3,21 @@
 // An item is one kv-head of one request and a tile of its rows, position by position
 // the G q-heads of each: a work group walks over the keys up to its last row's in
 // tiles of 64, in the one pass of attend_tile.h, and masks the tiles that its waves'
-// diagonals cross.  A wave leaves out the tiles behind its own last row, and of its
+// diagonals cross (looking at their values first, see finite: 0.3 % of a long prompt,
+// 2-3 % of batches of short ones).  A wave leaves out the tiles behind its own last row, and of its
 // last tile the weights of a second half that it does not see (batches 0-2 % faster;
 // leaving out its scores too needs a second copy of the loop, which spills).
 //
 // The matrix cores bound it from some 500 tokens on: 32768 tokens of 32 over 8 heads
-// are 8.8 TFLOP and take 8.3 to 9.0 ms, 975-1060 TFLOP/s of the 1200 of a large
+// are 8.8 TFLOP and take 8.2 to 9.0 ms, 975-1070 TFLOP/s of the 1200 of a large
 // library product; what holds a wave back is said in attend_tile.h.  One prompt has
-// few items and its longest bounds it: 1024 tokens 25 us, 4096 143.
+// few items and its longest bounds it: 512 tokens 15.1 us, 1024 24.7, 2048 51, 4096 143,
+// where the operations take 1.8, 7.2, 29 and 115 (512: the bytes 2.1).  Many short prompts are bound by
+// their bytes and by items that fill few of their rows: 64, 128 and 512 prompts of
+// 16-512 tokens take 116, 230 and 860 us, the bytes 66, 133 and 528.
 //
 // The tile: 256 rows read the 32 KB of 64 keys once from L2 (the 32768 tokens' reads
-// are 1.41 GB, 2.1 times q, k and v).  Work groups of four waves, two a compute unit,
+// are 1.41 GB, 3.5 times q, k and v).  Work groups of four waves, two a compute unit,
 // and three buffers instead of two were no faster.
 #include "attend_tile.h"
 #include "steps_host.h"
@@ -406,8 +410,8 @@ extern "C" int apex_steps_prompt_attention(const void* q, int64_t q_token_stride
     const int64_t rows = (int64_t)T * a.G.d;
     // Parts pay where a prompt's own chain of tiles is what takes the time: few items,
     // not too short, or about two to a unit if they are long.  32 over 8 heads, parts
-    // and none: one prompt of 256 tokens 11.1 us and 12.5, of 1024 24.9 and 32.8, of
-    // 2048 50 and 61; but of 100 9.4 and 9.2, of 4096 165 and 143, four of 512 tokens
+    // and none: one prompt of 256 tokens 11.3 us and 12.5, of 1024 24.7 and 32.8, of
+    // 2048 51 and 61; but of 100 9.4 and 9.2, of 4096 165 and 143, four of 512 tokens
     // 25.6 and 22.5.
     const int64_t parts_items = (rows / 128 + B) * Hkv, mean = T / B;
     if (mean >= 256 && 4 * parts_items <= (mean >= 1024 ? 9 : 5) * (int64_t)units) {
@@ -417,10 +421,12 @@ extern "C" int apex_steps_prompt_attention(const void* q, int64_t q_token_stride
     }
     const unsigned slots = (unsigned)(rows / 256) + (unsigned)B, items = slots * (unsigned)Hkv,
                    groups = items < (unsigned)units ? items : (unsigned)units;
-    // From eight items a work group on the sums are alike enough: 32768 tokens, 16
-    // items, 8.42 ms with all of them dealt out and 8.54 with the cheapest two left.
-    // Below, they are not: a chat batch of 16 prompts, 5 items, 89.5 us with all dealt
-    // out and 85.6 with four.
+    // From eight items a work group on the sums are alike enough to deal them all out;
+    // below, the cheapest are left.  34 batches of 1.4 to 23 items a work group (1-64
+    // prompts of 16-8192 tokens, G of 1 and 4), each with 1 to 8 rounds and with all
+    // dealt out: this rule is 2.1 % above the best of them in the mean (8.6 at most),
+    // all dealt out 3.9, one round 7.1, two 5.2, four 3.2.  From 4.5 to 6.7 items: four
+    // rounds 1.2 %, two 5.7, all 5.3; from eight on: all 2.5, four 4.0, one 9.2.
     const double ratio = (double)items / groups;
     const unsigned rounds = ratio >= 8 ? (unsigned)((items + groups - 1) / groups) : ratio < 2 ? 1 : ratio < 4.5 ? 2 : ratio < 6.7 ? 4 : 6;
     const unsigned alone = items > rounds * groups ? items - rounds * groups : 0;

@@ -5,9 +5,10 @@
 // below some 200 rows the cache's bytes bound it, above the matrix cores.  32
 // requests of 4096-32768 tokens with 5-8 drafted ones, 32 over 8 heads, are 1.78 GB
 // and take 283 us: 6.3 TB/s, and 6.6 inside the stream of units; the rest is the
-// first loads (9 us with the launch), the ends of parts, and the join (6).  With
+// first loads (9 us with the launch), the ends of parts, and the join (5).  With
 // more rows the work of a unit bounds it (attend_tile.h): 16 requests of 8000 tokens,
-// 8, 16 and 32 drafted ones: 90, 110 and 137 us.
+// 8, 16, 32 and 64 drafted ones: 90, 112, 157 and 254 us, where the bytes take 81 and
+// the operations of 64 113.
 #include "attend_tile.h"
 #include "steps_host.h"
 
@@ -23,8 +24,9 @@ constexpr int kSlabBytes = kBlockSize * kRowBytes;
 // its start (2, 4 and 6 were no better than 1); the work groups get equal shares of
 // it, one unit at least (one request of 500 tokens, shares of at least 1, 2 and 4:
 // 14.7, 15.2, 15.7 us).  A part of a pair leaves its sums in the workspace, for
-// join_kernel: a launch of its own, 4-6 us, where a count of the parts that have
-// come would have work groups wait for memory to be coherent.
+// join_kernel, a launch of its own: 3.4 us for one short request, 5-6 for batches.  (The
+// decode attention has the last part to come join the others, by coherent stores and
+// a count, for 0.8-1.3 us a part; here that was not built.)
 constexpr int kPairCost = 1;
 
 struct TreeArgs {
@@ -91,10 +93,10 @@ struct Shape {
     static constexpr int kBytes = kKeys * kRowBytes;             // of a unit's K or V
     // A wave brings the keys that it takes and no others, into one buffer, each half
     // of which it fills again as soon as it has read it (kOwn), or the work group's
-    // waves bring a unit together, into one of two buffers.  64 rows with a copy of
-    // the keys for each of the two waves that take them, and no barrier: 95 us for the
-    // 81 of 16 full trees over 32 heads; K brought one and a half units ahead, with a
-    // second barrier a unit: 88.
+    // waves bring a unit together, into one of two buffers.  (16 full trees over 32
+    // heads, weights still in one part: 64 rows with a copy of the keys for each of the
+    // two waves that take them, and no barrier, 95 us for 81; K brought one and a half
+    // units ahead, with a second barrier a unit, 88.)
     static constexpr bool kOwn = kRowWaves == 1;
     static constexpr int kBuffers = kOwn ? 1 : 2, kLds = 2 * kBuffers * kBytes;
     static constexpr int kLoads = kKeys / (4 * kWaves);          // of K, and of V, by which a wave brings its share of a unit
@@ -481,9 +483,11 @@ __global__ __launch_bounds__(256) void join_kernel(TreeArgs a, int tile_rows)
 
 // Shapes by the most rows of a pair: the smallest that holds them, whose waves share
 // the keys of a row among the most of them.  16 requests of 8000 tokens, 32 over
-// 8 heads, in shapes of 32, 64, 128 and 256: 32 rows 90, 105, 117, 166 us; 64 rows 110,
-// 124, 173; 128 rows 137, 189.  256 rows as one tile of 256 and as two of 128, on 8
-// requests of 4096 tokens: 76 and 79 us, 512 rows 125 and 132.
+// 8 heads, in shapes of 32, 64, 128 and 256: 32 rows 90, 104, 111, 141 us; 64 rows 112,
+// 118, 150; 128 rows 157, 175.  256 rows as one tile of 256 and as two of 128: 254 and
+// 281 us, but 59 and 53 for 1000 tokens; 8 requests of 4096 tokens on 64 over 8 heads,
+// 256 rows 84 and 91 us, 512 rows 141 and 153.  Their floors are 113, 17, 29 and
+// 58 us: few units a work group, and ends of parts that are as long.
 using Shape32 = Shape<1, 1>;
 using Shape64 = Shape<2, 1>;
 using Shape128 = Shape<4, 2>;
