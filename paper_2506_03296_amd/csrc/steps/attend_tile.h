@@ -57,6 +57,8 @@ constexpr float kLn2 = 0.69314718055994530942f;
 // ms for 32768 tokens.
 constexpr float kSlack = 4.0f;
 constexpr float kBias = 11.0f;
+// From here on c s and M are too coarse for 2^(c s - M) in one rounding, see nearer.
+constexpr float kFar = 1048576.0f;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
@@ -163,6 +165,7 @@ struct Rows {
     f32x16 o[4];         // O^T, dims 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4 in o[t][i], times 2^kBias
     float top;           // M
     float sum;           // of this lane's half of the keys
+    bool far;            // M of some row of the wave's is kFar or more in magnitude
 
     // Row pointer of the lane's query, or NULL: a row of zeros.
     __device__ void start(const char* row)
@@ -199,6 +202,7 @@ struct Rows {
             for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
         top = -INFINITY;
         sum = 0.0f;
+        far = false;
     }
 
     // Scores of the tiles' keys: key 32 u + 8 (i / 4) + 4 (lane / 32) + i % 4 in s[u][i].
@@ -251,10 +255,8 @@ struct Rows {
 
     // Weights of 32 keys' scores, as P^T's operands: keys 16 w + 4 half + 0..3 and + 8 in p[w].
     // kFine: p rounds towards 0, and `rest` has what is left.
-    __device__ void weights(const f32x16& s, float c, f16x8* p, f16x8* rest)
+    __device__ void weights(const f32x16& s, float c, float base, f16x8* p, f16x8* rest)
     {
-        // a row that has seen no score yet keeps M = -inf: 2^(-inf - 0) = 0
-        const float base = (top == -INFINITY ? 0.0f : top) - kBias;
         float part[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < 2; ++w)
@@ -288,6 +290,23 @@ struct Rows {
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[t][i] *= f;
         top = to;
+        far = __any(fabsf(to) >= kFar && to != -INFINITY);
+    }
+
+    // M to take scores from: a row that has seen none yet keeps M = -inf, and 2^(-inf - 0)
+    // is 0.
+    __device__ float from() const { return top == -INFINITY ? 0.0f : top; }
+
+    // Scores as their distance from M.  M is c times a score, rounded: c s - M in one
+    // rounding is off by as much, and far from 0 that is whole powers of 2, so that the
+    // largest weight itself would overflow or vanish.  With c s rounded as M was it is 0.
+    __device__ void nearer(f32x16 (&s)[kSub], float c) const
+    {
+#pragma clang fp contract(off)
+#pragma unroll
+        for (int u = 0; u < kSub; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[u][i] = s[u][i] * c - from();
     }
 
     // V^T's operand: dims 32 t + lane % 32, the 16 keys of step w in P^T's order.
@@ -337,16 +356,25 @@ struct Rows {
     // The weights of a unit's scores and their products with V: V's operands come
     // while weights are made, and the weights of 32 keys are made while the matrix
     // cores work on the 32 before them.  `half`: none of the second 32 is seen.
-    __device__ void take(const f32x16 (&s)[kSub], float c, const lds_char* v, bool half = false)
+    __device__ void take(f32x16 (&s)[kSub], float c, const lds_char* v, bool half = false)
     {
+        float base = 0.0f;
 #pragma unroll
         for (int u = 0; u < kSub; ++u) {
             if (u && half) break;
             f16x8 a[2][4];
             read_v(v, u, a);
-            if (u == 0) raise(s, c);
+            if (u == 0) {
+                raise(s, c);
+                base = from() - kBias;
+                if (__builtin_expect(far, 0)) {
+                    nearer(s, c);
+                    c = 1.0f;
+                    base = -kBias;
+                }
+            }
             f16x8 p[2], rest[2];
-            weights(s[u], c, p, rest);
+            weights(s[u], c, base, p, rest);
             add(a, p);
             if (kFine) add(a, rest);
         }
@@ -366,10 +394,14 @@ struct Rows {
             asm volatile("" ::: "memory");      // one load at a time: this path may not cost the other registers
         }
         dot = sum_of_halves(dot);
-        const float m = sees ? dot * c : -INFINITY;
-        if (__any(m > top + kSlack)) rescale(fmaxf(m, top));
-        const float base = (top == -INFINITY ? 0.0f : top) - kBias;
-        const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(dot, c, -base));
+        float at;
+        {
+#pragma clang fp contract(off)
+            const float m = sees ? dot * c : -INFINITY;
+            if (__any(m > top + kSlack)) rescale(fmaxf(m, top));
+            at = m - from();
+        }
+        const float e = __builtin_amdgcn_exp2f(at + kBias);
         if (!sees) return;
         if (half == 0) sum += e;
 #pragma unroll
